@@ -241,6 +241,60 @@ int cg_maxpool3x3s2(const void* x, void* y, int32_t n, int32_t h, int32_t wd, in
 int cg_avgpool_fc(const void* x, const void* wfc, const float* bias, float* logits, int32_t n, int32_t hw, int32_t c,
                   int32_t classes, void* hip_stream);
 
+/*
+ * What is done with the logits behind the classifier.  logits: [rows] rows of `classes` elements, dtype CG_F32 or
+ * CG_BF16, `row_stride` elements from one row to the next (any, 0 too: every row the same), aligned to their elements only.
+ * Class indices are int64.  All pointers are DEVICE pointers, nothing is allocated, work is only enqueued on hip_stream, and
+ * arguments are checked before any HIP call.  Sums are held in fp32, whatever the logits' type, and added in an order that
+ * depends on the sizes of the call alone: the same call gives the same bits.  A workspace may be NULL where its size is 0, else it is
+ * 256-byte aligned; a captured call keeps its address, so it must stay the graph's own, and calls that may overlap need
+ * workspaces of their own.  Outputs must not overlap inputs or each other, but for `grad`, which may be the logits
+ * themselves, with their strides.
+ */
+enum { CG_TOP_MAX = 128 }; /* the most alternatives, and the most classes of a teacher, per row */
+
+/* Log probabilities log p = log softmax(logits / temperature), temperature > 0:
+ *   logprob       [rows][given]: those of the classes labels[rows][given].  A negative label is absent: 0; one of `classes`
+ *                 or more gives NaN.  Not touched if given == 0 (both nullable then).
+ *   entropy       nullable, [rows]: -sum p log p
+ *   top_ids, top_logprobs  [rows][top]: the `top` classes of the greatest logits in falling order, equal ones (0 and -0 too) by
+ *                 rising index; 0 <= top <= min(classes, CG_TOP_MAX); nullable if top == 0
+ * A class of -inf has probability 0 (log -inf).  A row of -inf throughout has log probabilities -inf, entropy 0 and its first
+ * classes as alternatives.  A row with a NaN or +inf has no distribution: NaN in the place of log probabilities (other than those of
+ * absent labels) and entropy, -1 in the place of top_ids. */
+size_t cg_logprobs_workspace_bytes(int64_t rows, int32_t classes, int32_t top);
+int cg_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t classes, int64_t row_stride, float temperature,
+                const int64_t* labels, int32_t given, int32_t top, float* logprob, float* entropy, int64_t* top_ids,
+                float* top_logprobs, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits (the paper's training uses a teacher with both terms at equal weight and temperature 1), per row
+ *   loss = label_weight * -log p1[label]  +  teacher_weight * sum_j q[j] * (log q[j] - log pT[top_ids[j]])
+ * with p1 = softmax(logits), pT = softmax(logits / temperature) over all classes and q = softmax(top_logits / temperature)
+ * over the row's `top` teacher classes (any constant may be added to a row of top_logits: log probabilities will do).
+ *   top_ids, top_logits  [rows][top], top <= CG_TOP_MAX.  A negative id is absent; so lists may be ragged.  A class named twice counts
+ *                 with both entries.  top_logits of -inf hold no mass.  Nullable if top == 0 (teacher_weight must then be 0).
+ *   labels        [rows], negative: absent.  Nullable if label_weight is 0.
+ * A term whose weight is 0, whose label is absent or whose teacher has no mass is left out of its row.  A row without terms, and a row of
+ * -inf throughout, has loss 0 and gradient 0, whatever else it holds.  A label or id of `classes` or more makes the loss and the
+ * gradient of its row NaN, as do NaN and +inf among the logits or the top_logits of a term that the row has.  A class of -inf that the row's label or teacher
+ * asks for makes the loss +inf.
+ *   loss          [rows]
+ *   stats         nullable, [rows][3]: the greatest logit m, sum exp(logits - m) and sum exp((logits - m) / temperature), which
+ *                 cg_distill_backward takes; a sum that the call has no use for (its term's weight is 0) may be NaN
+ *   grad          nullable, logits' dtype, rows of grad_stride >= classes elements: grad_loss[row] * d loss / d logits, rounded once;
+ *                 elements between the rows are left as they were
+ *   grad_loss     nullable (= 1), [rows]: the gradient that comes from above; used with grad only
+ * cg_distill_backward forms the same gradient from stats, logits, teacher and weights as they were in the forward call. */
+size_t cg_distill_workspace_bytes(int64_t rows, int32_t classes);
+int cg_distill_forward(const void* logits, int32_t dtype, int64_t rows, int32_t classes, int64_t row_stride, float temperature,
+                       const int64_t* top_ids, const float* top_logits, int32_t top, const int64_t* labels, float teacher_weight,
+                       float label_weight, float* loss, float* stats, const float* grad_loss, void* grad, int64_t grad_stride,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+int cg_distill_backward(const void* logits, int32_t dtype, int64_t rows, int32_t classes, int64_t row_stride, float temperature,
+                        const int64_t* top_ids, const float* top_logits, int32_t top, const int64_t* labels, float teacher_weight,
+                        float label_weight, const float* stats, const float* grad_loss, void* grad, int64_t grad_stride,
+                        void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

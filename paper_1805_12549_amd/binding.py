@@ -85,7 +85,9 @@ CG_VARIANT_AUTO, CG_VARIANT_NAIVE, CG_VARIANT_MFMA_ROWS, CG_VARIANT_TILE = 0, 1,
 EXPORTS = ("cg_conv_packed_bytes", "cg_conv_create", "cg_conv_workspace_bytes", "cg_conv_forward",
            "cg_conv_forward_noalloc",
            "cg_conv_destroy", "cg_conv_info", "cg_last_error", "cg_small_cin_conv", "cg_conv7x7s2_maxpool", "cg_pointwise_conv",
-           "cg_maxpool3x3s2", "cg_avgpool_fc")
+           "cg_maxpool3x3s2", "cg_avgpool_fc", "cg_logprobs_workspace_bytes", "cg_logprobs", "cg_distill_workspace_bytes", "cg_distill_forward",
+           "cg_distill_backward")
+CG_TOP_MAX = 128
 
 _pf = C.POINTER(C.c_float)
 _pi = C.POINTER(C.c_int32)
@@ -141,6 +143,18 @@ _lib.cg_maxpool3x3s2.argtypes = [C.c_void_p, C.c_void_p] + [C.c_int32] * 4 + [C.
 _lib.cg_maxpool3x3s2.restype = C.c_int
 _lib.cg_avgpool_fc.argtypes = [C.c_void_p] * 4 + [C.c_int32] * 4 + [C.c_void_p]
 _lib.cg_avgpool_fc.restype = C.c_int
+_logits_args = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_float]
+_teacher_args = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_float, C.c_float]
+_lib.cg_logprobs_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32]
+_lib.cg_logprobs_workspace_bytes.restype = C.c_size_t
+_lib.cg_logprobs.argtypes = _logits_args + [C.c_void_p, C.c_int32, C.c_int32] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+_lib.cg_logprobs.restype = C.c_int
+_lib.cg_distill_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
+_lib.cg_distill_workspace_bytes.restype = C.c_size_t
+_lib.cg_distill_forward.argtypes = _logits_args + _teacher_args + [C.c_void_p] * 4 + [C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.cg_distill_forward.restype = C.c_int
+_lib.cg_distill_backward.argtypes = _logits_args + _teacher_args + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p]
+_lib.cg_distill_backward.restype = C.c_int
 
 
 def current_stream_ptr() -> int:
@@ -228,6 +242,36 @@ def cg_avgpool_fc(x: int, wfc: int, bias: int, logits: int, n: int, hw: int, c: 
                   hip_stream: int = 0) -> None:
     _check(_lib.cg_avgpool_fc(x, wfc, bias, logits, n, hw, c, classes,
                               hip_stream))
+
+
+def cg_logprobs_workspace_bytes(rows: int, classes: int, top: int) -> int:
+    return int(_lib.cg_logprobs_workspace_bytes(rows, classes, top))
+
+
+def cg_logprobs(logits: int, dtype: int, rows: int, classes: int, row_stride: int, temperature: float, labels: int, given: int,
+                top: int, logprob: int, entropy: int, top_ids: int, top_logprobs: int, workspace: int, workspace_bytes: int,
+                hip_stream: int = 0) -> None:
+    """Raw device addresses (0 = NULL)."""
+    _check(_lib.cg_logprobs(logits, dtype, rows, classes, row_stride, temperature, labels, given, top, logprob, entropy, top_ids,
+                            top_logprobs, workspace, workspace_bytes, hip_stream))
+
+
+def cg_distill_workspace_bytes(rows: int, classes: int) -> int:
+    return int(_lib.cg_distill_workspace_bytes(rows, classes))
+
+
+def cg_distill_forward(logits: int, dtype: int, rows: int, classes: int, row_stride: int, temperature: float, top_ids: int,
+                       top_logits: int, top: int, labels: int, teacher_weight: float, label_weight: float, loss: int, stats: int,
+                       grad_loss: int, grad: int, grad_stride: int, workspace: int, workspace_bytes: int, hip_stream: int = 0) -> None:
+    _check(_lib.cg_distill_forward(logits, dtype, rows, classes, row_stride, temperature, top_ids, top_logits, top, labels, teacher_weight,
+                                   label_weight, loss, stats, grad_loss, grad, grad_stride, workspace, workspace_bytes, hip_stream))
+
+
+def cg_distill_backward(logits: int, dtype: int, rows: int, classes: int, row_stride: int, temperature: float, top_ids: int,
+                        top_logits: int, top: int, labels: int, teacher_weight: float, label_weight: float, stats: int, grad_loss: int,
+                        grad: int, grad_stride: int, hip_stream: int = 0) -> None:
+    _check(_lib.cg_distill_backward(logits, dtype, rows, classes, row_stride, temperature, top_ids, top_logits, top, labels, teacher_weight,
+                                    label_weight, stats, grad_loss, grad, grad_stride, hip_stream))
 
 
 def empty_beside(x, *sizes, dtype=torch.bfloat16):
@@ -404,3 +448,142 @@ class GatedConv:
             self.close()
         except Exception:
             pass
+
+
+# ----------------------------------------------------------------------------
+# The operators behind the classifier, on tensors.  Still marshalling only.
+# ----------------------------------------------------------------------------
+
+_LOGITS = {torch.float32: CG_F32, torch.bfloat16: CG_BF16}
+
+
+def _refuse(name: str, why: str, code: int = CG_EINVAL):
+    raise CGError(code, "%s: %s" % (name, why))
+
+
+def _logits_of(name, logits):
+    """(dtype, rows, classes, elements between rows) of a 2-d tensor on the current device."""
+    dtype = _LOGITS.get(logits.dtype)
+    if dtype is None:
+        _refuse(name, "logits are float32 or bfloat16", CG_EUNSUPPORTED)
+    if logits.dim() != 2:
+        _refuse(name, "logits are [rows, classes]")
+    if not logits.is_cuda or logits.get_device() != _current_device():
+        _refuse(name, "logits must be on the current device")
+    (rows, classes), (stride, step) = logits.shape, logits.stride()
+    if step != 1 and classes > 1:
+        _refuse(name, "the classes of a row must lie side by side")
+    return dtype, rows, classes, stride
+
+
+def _beside(name, what, t, dtype, shape, device):
+    """The address of a contiguous tensor of that type and shape on `device`; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _refuse(name, "%s must be a contiguous %s tensor of shape %s beside the logits" % (what, str(dtype)[6:], tuple(shape)))
+    return t.data_ptr()
+
+
+def logprobs(logits, labels=None, top: int = 0, temperature: float = 1.0, entropy: bool = True):
+    """Log probabilities log softmax(logits / temperature): (logprob, entropy, top_ids, top_logprobs), None for what is not asked for.
+
+    logits: [rows, classes], float32 or bfloat16, any distance between rows.  labels: int64 [rows] or [rows, given], the classes whose log
+    probability is wanted (logprob has their shape; negative: absent, 0).  top: so many alternatives per row in falling order, equal ones by
+    index (int64 and float32 [rows, top]).  entropy: float32 [rows].  See cg_logprobs in cg_conv.h for rows of -inf, NaN and +inf."""
+    dtype, rows, classes, stride = _logits_of("logprobs", logits)
+    dev = logits.device
+    given, logprob, given_entropy, top_ids, top_logprobs = 0, None, None, None, None
+    if labels is not None:
+        if labels.dim() not in (1, 2) or labels.shape[0] != rows:
+            _refuse("logprobs", "labels are [rows] or [rows, given]")
+        given = 1 if labels.dim() == 1 else labels.shape[1]
+        logprob = _empty(labels.shape, dtype=torch.float32, device=dev)
+    labels_ptr = _beside("logprobs", "labels", labels, torch.int64, None if labels is None else labels.shape, dev)
+    if not 0 <= top <= classes:
+        _refuse("logprobs", "top lies in [0, classes]")
+    if top:
+        top_ids = _empty((rows, top), dtype=torch.int64, device=dev)
+        top_logprobs = _empty((rows, top), dtype=torch.float32, device=dev)
+    if entropy:
+        given_entropy = _empty(rows, dtype=torch.float32, device=dev)
+    stream = _raw_stream(_current_device())
+    need = _lib.cg_logprobs_workspace_bytes(rows, classes, top)
+    ws = _raw_alloc(need, stream) if need else 0        # (as in GatedConv.forward: the call's own, or the graph's)
+    try:
+        rc = _lib.cg_logprobs(logits.data_ptr(), dtype, rows, classes, stride, temperature, labels_ptr, given, top,
+                              0 if logprob is None else logprob.data_ptr(), 0 if given_entropy is None else given_entropy.data_ptr(),
+                              0 if top_ids is None else top_ids.data_ptr(), 0 if top_logprobs is None else top_logprobs.data_ptr(), ws, need, stream)
+    finally:
+        if ws:
+            _raw_free(ws)
+    _check(rc)
+    return logprob, given_entropy, top_ids, top_logprobs
+
+
+def _teacher_of(name, logits, rows, top_ids, top_logits, labels):
+    if (top_ids is None) != (top_logits is None):
+        _refuse(name, "top_ids and top_logits come together")
+    top = 0
+    if top_ids is not None:
+        if top_ids.dim() != 2 or top_ids.shape[0] != rows:
+            _refuse(name, "top_ids and top_logits are [rows, top]")
+        top = top_ids.shape[1]
+    shape, dev = (rows, top), logits.device
+    return (_beside(name, "top_ids", top_ids, torch.int64, shape, dev), _beside(name, "top_logits", top_logits, torch.float32, shape, dev), top,
+            _beside(name, "labels", labels, torch.int64, (rows,), dev))
+
+
+def _grad_of(name, logits, grad, rows, classes, stride):
+    """The tensor that takes the gradient: a given one, or a new one whose rows are aligned to 16 bytes as the logits' are."""
+    if grad is None or grad is True:
+        return _strided((rows, classes), (classes + (stride - classes) % (16 // logits.element_size()), 1), dtype=logits.dtype, device=logits.device)
+    if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device or (grad.stride(1) != 1 and classes > 1):
+        _refuse(name, "grad must be of the logits' type and shape beside them, the classes of a row side by side")
+    return grad
+
+
+def distill(logits, top_ids, top_logits, labels=None, *, teacher_weight: float = 1.0, label_weight: float = 0.0, temperature: float = 1.0,
+            grad=None, grad_loss=None):
+    """Distillation from a teacher's top logits: (loss, stats, grad), one loss per row:
+    label_weight * -log softmax(logits)[label] + teacher_weight * KL(softmax(top_logits / temperature) || softmax(logits / temperature)).
+
+    logits: [rows, classes], float32 or bfloat16, any distance between rows.  top_ids, top_logits: int64 and float32 [rows, top], negative ids
+    are absent (both may be None with teacher_weight=0).  labels: int64 [rows], negative: absent.  grad=True: the gradient with respect to the
+    logits as well, in the same call (a tensor: into that one, the logits themselves too), times grad_loss (float32 [rows], None: 1).
+    stats: what distill_backward takes for the same gradient later on.  The usual factor temperature^2 is the caller's to put into
+    teacher_weight.  See cg_distill_forward in cg_conv.h for rows of -inf, NaN and +inf and for labels and ids outside the classes."""
+    name = "distill"
+    dtype, rows, classes, stride = _logits_of(name, logits)
+    ids_ptr, top_ptr, top, labels_ptr = _teacher_of(name, logits, rows, top_ids, top_logits, labels)
+    up_ptr = _beside(name, "grad_loss", grad_loss, torch.float32, (rows,), logits.device)
+    want = grad is not None and grad is not False
+    grad = _grad_of(name, logits, grad, rows, classes, stride) if want else None
+    loss = _empty(rows, dtype=torch.float32, device=logits.device)
+    stats = _empty((rows, 3), dtype=torch.float32, device=logits.device)
+    stream = _raw_stream(_current_device())
+    need = _lib.cg_distill_workspace_bytes(rows, classes)
+    ws = _raw_alloc(need, stream) if need else 0
+    try:
+        rc = _lib.cg_distill_forward(logits.data_ptr(), dtype, rows, classes, stride, temperature, ids_ptr, top_ptr, top, labels_ptr, teacher_weight,
+                                     label_weight, loss.data_ptr(), stats.data_ptr(), up_ptr, grad.data_ptr() if want else 0,
+                                     grad.stride(0) if want else 0, ws, need, stream)
+    finally:
+        if ws:
+            _raw_free(ws)
+    _check(rc)
+    return loss, stats, grad
+
+
+def distill_backward(logits, stats, top_ids, top_logits, labels=None, *, teacher_weight: float = 1.0, label_weight: float = 0.0,
+                     temperature: float = 1.0, grad=None, grad_loss=None):
+    """The gradient of distill's losses with respect to the logits, times grad_loss, from the stats of the forward call and its arguments."""
+    name = "distill_backward"
+    dtype, rows, classes, stride = _logits_of(name, logits)
+    ids_ptr, top_ptr, top, labels_ptr = _teacher_of(name, logits, rows, top_ids, top_logits, labels)
+    stats_ptr = _beside(name, "stats", stats, torch.float32, (rows, 3), logits.device)
+    up_ptr = _beside(name, "grad_loss", grad_loss, torch.float32, (rows,), logits.device)
+    grad = _grad_of(name, logits, grad, rows, classes, stride)
+    _check(_lib.cg_distill_backward(logits.data_ptr(), dtype, rows, classes, stride, temperature, ids_ptr, top_ptr, top, labels_ptr, teacher_weight,
+                                    label_weight, stats_ptr, up_ptr, grad.data_ptr(), grad.stride(0), _raw_stream(_current_device())))
+    return grad
