@@ -43,9 +43,6 @@ struct Sum {
 struct Max {
   __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
-struct MaxKey {
-  __device__ uint64_t operator()(uint64_t a, uint64_t b) const { return a > b ? a : b; }
-};
 
 // over the workgroup, in an order that does not change; `part` (kWaves values) may be used again after the next barrier
 template <class V, class Op>
@@ -61,6 +58,149 @@ __device__ __forceinline__ V over_workgroup(V v, V* part, Op op) {
   return v;
 }
 
+// exp2 by the hardware (one ulp; results below 2^-126 are 0)
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row as the lanes of a workgroup walk it: elements in front of the first 16-byte boundary, whole 16-byte chunks, elements behind the last one.
+template <class T>
+struct RowSpan {
+  static constexpr int kPer = 16 / (int)sizeof(T);      // elements of a chunk
+  const T* z;
+  const uint4* body;
+  int head, chunks, tail_from, classes;
+  __device__ RowSpan(const T* row, int n) : z(row), classes(n) {
+    const int lead = (int)((0 - (uintptr_t)row) & 15) / (int)sizeof(T);
+    head = lead < n ? lead : n;
+    chunks = (n - head) / kPer;
+    body = (const uint4*)(row + head);
+    tail_from = head + chunks * kPer;
+  }
+  // the element beside the chunks that lane `tid` takes (fewer than 16 in all), or -1
+  __device__ int beside(int tid) const {
+    const int v = tid < head ? tid : tail_from + tid - head;
+    return v < (tid < head ? head : classes) ? v : -1;
+  }
+};
+
+__device__ __forceinline__ void unpack(const uint4& c, float* x, const float*) {
+  x[0] = __uint_as_float(c.x), x[1] = __uint_as_float(c.y), x[2] = __uint_as_float(c.z), x[3] = __uint_as_float(c.w);
+}
+__device__ __forceinline__ void unpack(const uint4& c, float* x, const uint16_t*) {
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+}
+template <class T>
+__device__ __forceinline__ uint4 all_minus_inf() {
+  const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  return make_uint4(w, w, w, w);
+}
+
+constexpr float kLeast = -1.0e4f;     // in the place of exponents from there down to -inf, whose power is 0, where they are factors of it
+
+// A softmax in one pass: with m the greatest logit so far, the sum of e = 2^((z - m) c) and the sum of e (z - m) c, c = log2(e) / temperature.
+// A new maximum scales both.  NaN and +inf make the sum NaN; without any class m is -inf and the sum 0.
+struct Online {
+  float m, sum, moment;
+  // to the maximum `to` >= m
+  __device__ void raise(float to, float c) {
+    const float d = fmaxf((m - to) * c, kLeast), f = pow2(d);
+    moment = f * (moment + d * sum);
+    sum *= f;
+    m = to;
+  }
+  template <int N>
+  __device__ void take(const float* x, float most, float c) {
+    if (most > m) raise(most, c);
+    const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float y = (x[i] - from) * c, e = pow2(y);
+      sum += e;
+      moment = fmaf(e, fmaxf(y, kLeast), moment);
+    }
+  }
+  __device__ void join(const Online& o, float c) {
+    Online b = o;
+    const float to = fmaxf(m, b.m);
+    raise(to, c);
+    b.raise(to, c);
+    sum += b.sum;
+    moment += b.moment;
+  }
+};
+
+// over the workgroup; every thread gets the result.  `part`: one value for each wavefront, free again after the next barrier
+__device__ __forceinline__ Online over_workgroup(Online o, Online* part, float c) {
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) {
+    Online b;
+    b.m = __shfl_xor(o.m, s, 64);
+    b.sum = __shfl_xor(o.sum, s, 64);
+    b.moment = __shfl_xor(o.moment, s, 64);
+    o.join(b, c);
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = o;
+  __syncthreads();
+  o = part[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) o.join(part[w], c);
+  return o;
+}
+
+constexpr int kUnroll = 4;           // chunks that a lane has on their way
+constexpr int kMarks = 16;           // stretches of a lane whose greatest logits are kept
+constexpr int kCandidates = 1024;    // at most so many are compared with each other
+
+struct TopLds {
+  float mark[kMarks][kThreads];      // of each lane's stretches
+  alignas(16) uint64_t lane_key[kThreads];
+  alignas(16) uint64_t found[kCandidates];
+  uint64_t bound;
+  int count;
+};
+
+// how many of keys[0, n) come before `key`, the entry `at`
+__device__ __forceinline__ int rank_among(const uint64_t* keys, int n, uint64_t key, int at) {
+  int r = 0;
+  int j = 0;
+  for (; j + 2 <= n; j += 2) {
+    const ulonglong2 k = *(const ulonglong2*)(keys + j);
+    r += (k.x > key || (k.x == key && j < at)) + (k.y > key || (k.y == key && j + 1 < at));
+  }
+  if (j < n) r += keys[j] > key || (keys[j] == key && j < at);
+  return r;
+}
+
+// The `top` greatest keys of a workgroup's lanes: found[0, n) holds them, and few others.  `mine` is not above the greatest key of this lane (0: it
+// has none), scan(bound) puts every key of this lane from `bound` up into `found`.  The top-th of the lanes' own is a bound that at least
+// `top` keys reach; as a rule few more do.  Where `found` does not hold them (equal logits, or a lane that has many of the greatest), the
+// top-th of those that it took, whichever these are, is a higher bound that `top` keys reach, and at least kCandidates - top keys lie below it.
+template <class Scan>
+__device__ int find_top(TopLds& l, uint64_t mine, int top, Scan scan) {
+  const int tid = (int)threadIdx.x;
+  __syncthreads();
+  l.lane_key[tid] = mine;
+  __syncthreads();
+  if (rank_among(l.lane_key, kThreads, mine, tid) == top - 1) l.bound = mine;
+  for (;;) {
+    if (tid == 0) l.count = 0;
+    __syncthreads();
+    scan(l.bound);
+    __syncthreads();
+    const int n = l.count;
+    if (n <= kCandidates) return n;
+    for (int i = tid; i < kCandidates; i += kThreads)
+      if (rank_among(l.found, kCandidates, l.found[i], i) == top - 1) l.bound = l.found[i];
+    __syncthreads();
+  }
+}
+__device__ __forceinline__ void add_found(TopLds& l, uint64_t key) {
+  const int at = atomicAdd(&l.count, 1);
+  if (at < kCandidates) l.found[at] = key;
+}
+
 struct LogprobArgs {
   const void* logits;
   long long rows, stride;
@@ -72,46 +212,87 @@ struct LogprobArgs {
   float* top_logprobs;
 };
 
+// One pass over the row (V elements are read once): every lane keeps its own running maximum and sums.  The alternatives come from what the pass
+// leaves behind: the lanes' maxima give a bound that is reached by little more than `top` classes, the maxima of each lane's stretches say where those
+// lie, and only such stretches are read again.
 template <class T>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
-  __shared__ float part[kWaves];
-  __shared__ uint64_t part_key[kWaves];
+  __shared__ Online part[kWaves];
+  __shared__ TopLds top;
+  constexpr int N = RowSpan<T>::kPer;
   const int tid = (int)threadIdx.x;
+  const float c = a.scale * kLog2E;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* z = (const T*)a.logits + row * a.stride;
-    float m = -INFINITY;
-    for (long long v = tid; v < a.classes; v += kThreads) m = fmaxf(m, as_float(z[v]));
-    m = over_workgroup(m, part, Max());
-    const float from = m == -INFINITY ? 0.0f : m;      // (a row without a class: exponentials of -inf, no NaN)
-    float sum = 0.0f, moment = 0.0f;                    // of e, and of e times its exponent
-    for (long long v = tid; v < a.classes; v += kThreads) {
-      const float y = (as_float(z[v]) - from) * a.scale, e = exp2f(y * kLog2E);
-      sum += e;
-      moment += e > 0.0f ? e * y : e;                   // (NaN stays)
+    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes);
+    const int groups = (z.chunks + kThreads * kUnroll - 1) / (kThreads * kUnroll);
+    const int per_mark = (groups + kMarks - 1) / kMarks;       // groups of a stretch
+    const int extra = z.beside(tid);
+    Online o{-INFINITY, 0.0f, 0.0f};
+    const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
+    float stretch = -INFINITY;
+    for (int g = 0, in = 0, mark = 0; g < groups; ++g) {
+      uint4 raw[kUnroll];
+      const int at = g * kThreads * kUnroll + tid;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
+      float x[kUnroll * N], most = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
+#pragma unroll
+      for (int i = 0; i < kUnroll * N; ++i) most = fmaxf(most, x[i]);
+      o.take<kUnroll * N>(x, most, c);
+      stretch = fmaxf(stretch, most);
+      if (++in == per_mark || g + 1 == groups) {
+        if (a.top) top.mark[mark][tid] = stretch;
+        stretch = -INFINITY;
+        in = 0;
+        ++mark;
+      }
     }
-    sum = over_workgroup(sum, part, Sum());
-    moment = over_workgroup(moment, part, Sum());
-    const bool none = sum == 0.0f, bad = sum != sum;
-    const float log_sum = logf(sum);
-    const auto logprob = [&](float x) { return none ? -INFINITY : bad ? NAN : (x - m) * a.scale - log_sum; };
+    o.take<1>(&x0, x0, c);
+    const bool holds = tid < z.chunks || extra >= 0;
+    const uint64_t mine = holds ? rank_key(o.m, ~0u) : 0;
+    o = over_workgroup(o, part, c);
+    const bool none = o.sum == 0.0f, bad = o.sum != o.sum;
+    const float log_sum = logf(o.sum);
+    const auto logprob = [&](float x) { return none ? -INFINITY : bad ? NAN : (x - o.m) * a.scale - log_sum; };
     for (int g = tid; g < a.given; g += kThreads) {
       const int64_t id = a.labels[row * a.given + g];
-      a.logprob[row * a.given + g] = id < 0 ? 0.0f : id >= a.classes ? NAN : logprob(as_float(z[id]));
+      a.logprob[row * a.given + g] = id < 0 ? 0.0f : id >= a.classes ? NAN : logprob(as_float(z.z[id]));
     }
-    if (a.entropy && tid == 0) a.entropy[row] = none ? 0.0f : log_sum - moment / sum;
-    uint64_t last = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-      uint64_t best = 0;
-      for (long long v = tid; v < a.classes && !bad; v += kThreads) {
-        const uint64_t key = rank_key(as_float(z[v]), (uint32_t)v);
-        if (key < last && key > best) best = key;
+    if (a.entropy && tid == 0) a.entropy[row] = none ? 0.0f : log_sum - o.moment / (o.sum * kLog2E);
+    if (!a.top) continue;
+    if (bad) {
+      if (tid < a.top) {
+        a.top_ids[row * a.top + tid] = -1;
+        a.top_logprobs[row * a.top + tid] = NAN;
       }
-      last = over_workgroup(best, part_key, MaxKey());
-      if (tid == 0) {
-        const uint32_t id = ~(uint32_t)last;
-        a.top_ids[row * a.top + k] = bad ? -1 : (int64_t)id;
-        a.top_logprobs[row * a.top + k] = bad ? NAN : logprob(as_float(z[id]));
+      continue;
+    }
+    const int n = find_top(top, mine, a.top, [&](uint64_t bound) {
+      const auto offer = [&](float x, int v) {
+        const uint64_t key = rank_key(x, (uint32_t)v);
+        if (key >= bound) add_found(top, key);
+      };
+      if (extra >= 0) offer(x0, extra);
+      for (int mark = 0; mark * per_mark < groups; ++mark) {
+        if (rank_key(top.mark[mark][tid], 0) < bound) continue;
+        const int g1 = (mark + 1) * per_mark < groups ? (mark + 1) * per_mark : groups;
+        for (int ch = mark * per_mark * kThreads * kUnroll + tid; ch < g1 * kThreads * kUnroll && ch < z.chunks; ch += kThreads) {
+          float x[N];
+          unpack(z.body[ch], x, (const T*)nullptr);
+#pragma unroll
+          for (int i = 0; i < N; ++i) offer(x[i], z.head + ch * N + i);
+        }
       }
+    });
+    for (int i = tid; i < n; i += kThreads) {
+      const uint64_t key = top.found[i];
+      const int r = rank_among(top.found, n, key, i);
+      if (r >= a.top) continue;
+      const uint32_t id = ~(uint32_t)key;
+      a.top_ids[row * a.top + r] = (int64_t)id;
+      a.top_logprobs[row * a.top + r] = logprob(as_float(z.z[id]));
     }
   }
 }
