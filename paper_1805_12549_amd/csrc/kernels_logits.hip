@@ -37,27 +37,6 @@ __device__ __forceinline__ uint64_t rank_key(float z, uint32_t index) {
   return ((uint64_t)up << 32) | (uint32_t)~index;
 }
 
-struct Sum {
-  __device__ float operator()(float a, float b) const { return a + b; }
-};
-struct Max {
-  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
-};
-
-// over the workgroup, in an order that does not change; `part` (kWaves values) may be used again after the next barrier
-template <class V, class Op>
-__device__ __forceinline__ V over_workgroup(V v, V* part, Op op) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) v = op(v, (V)__shfl_xor(v, s, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) v = op(v, part[w]);
-  return v;
-}
-
 // exp2 by the hardware (one ulp; results below 2^-126 are 0)
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -312,89 +291,216 @@ struct DistillArgs {
   void* grad;
 };
 
+// The teacher's side of a row and the logits that its terms ask for, taken by the first wavefront while the others start on the row.
+struct TeacherLds {
+  int64_t id[CG_TOP_MAX];        // -1: absent
+  float q[CG_TOP_MAX], log_q[CG_TOP_MAX], z[CG_TOP_MAX];
+  float mass, z_label;
+  int beyond;                    // an id names no class
+};
+
 template <class T>
+__device__ __forceinline__ void take_teacher(TeacherLds& l, const DistillArgs& a, long long row, const T* z, int64_t label) {
+  const int lane = (int)threadIdx.x;
+  constexpr int kEach = CG_TOP_MAX / 64;
+  int64_t id[kEach];
+  float t[kEach], most = -INFINITY, mass = 0.0f;
+  bool beyond = false;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int at = lane + 64 * k;
+    id[k] = at < a.top ? a.top_ids[row * a.top + at] : -1;
+    t[k] = id[k] >= 0 ? a.top_logits[row * a.top + at] : -INFINITY;
+    most = fmaxf(most, t[k]);
+    beyond |= id[k] >= a.classes;
+  }
+  if (lane == 0) l.z_label = label >= 0 && label < a.classes ? as_float(z[label]) : 0.0f;
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) most = fmaxf(most, __shfl_xor(most, s, 64));
+  if (most == -INFINITY) most = 0.0f;
+  float e[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    t[k] = (t[k] - most) * a.scale;
+    e[k] = pow2(t[k] * kLog2E);
+    mass += e[k];
+  }
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) mass += __shfl_xor(mass, s, 64);
+  const float log_mass = logf(mass);
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int at = lane + 64 * k;
+    if (at >= a.top) continue;
+    l.id[at] = id[k];
+    l.q[at] = mass != 0.0f ? e[k] / mass : 0.0f;
+    l.log_q[at] = t[k] - log_mass;
+    l.z[at] = id[k] >= 0 && id[k] < a.classes ? as_float(z[id[k]]) : 0.0f;
+  }
+  if (lane == 0) l.mass = mass;
+  beyond = __any(beyond);
+  if (lane == 0) l.beyond = beyond;
+}
+
+// A row's sums for the one or two temperatures of a call: m the greatest logit, `sum` of 2^((z - m) c), `sum1` (TWO) of 2^((z - m) log2 e).
+template <bool TWO>
+struct Sums {
+  float m, sum, sum1;
+  __device__ void raise(float to, float c) {
+    sum *= pow2(fmaxf((m - to) * c, kLeast));
+    if (TWO) sum1 *= pow2(fmaxf((m - to) * kLog2E, kLeast));
+    m = to;
+  }
+  template <int N>
+  __device__ void take(const float* x, float most, float c) {
+    if (most > m) raise(most, c);
+    const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      sum += pow2((x[i] - from) * c);
+      if (TWO) sum1 += pow2((x[i] - from) * kLog2E);
+    }
+  }
+  __device__ void join(Sums b, float c) {
+    const float to = fmaxf(m, b.m);
+    raise(to, c);
+    b.raise(to, c);
+    sum += b.sum;
+    if (TWO) sum1 += b.sum1;
+  }
+};
+template <bool TWO>
+__device__ __forceinline__ Sums<TWO> over_workgroup(Sums<TWO> o, Sums<TWO>* part, float c) {
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) {
+    Sums<TWO> b;
+    b.m = __shfl_xor(o.m, s, 64);
+    b.sum = __shfl_xor(o.sum, s, 64);
+    b.sum1 = TWO ? __shfl_xor(o.sum1, s, 64) : 0.0f;
+    o.join(b, c);
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = o;
+  __syncthreads();
+  o = part[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) o.join(part[w], c);
+  return o;
+}
+
+__device__ __forceinline__ uint4 pack(const float* g, const float*) {
+  return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+}
+__device__ __forceinline__ uint4 pack(const float* g, const uint16_t*) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)float_to_bf16(g[2 * i]) | (uint32_t)float_to_bf16(g[2 * i + 1]) << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Loss and gradient of a row.  One pass for the sums (none where the call brings them), one that writes the gradient: for every class the
+// probabilities' part; then the classes that the label or the teacher names are written again, in full and rounded once.  TWO: both terms
+// are there at different temperatures, that is two sums and two exponentials an element.
+template <class T, bool TWO>
 __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
-  __shared__ float part[kWaves];
-  __shared__ float mass_of[CG_TOP_MAX];
-  __shared__ int64_t id_of[CG_TOP_MAX];
+  __shared__ Sums<TWO> part[kWaves];
+  __shared__ TeacherLds teacher;
+  constexpr int N = RowSpan<T>::kPer;
   const int tid = (int)threadIdx.x;
+  const float c = a.w_teacher != 0.0f ? a.scale * kLog2E : kLog2E;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* z = (const T*)a.logits + row * a.stride;
-    T* g = a.grad ? (T*)a.grad + row * a.grad_stride : nullptr;
-    // the teacher's distribution: one entry a thread
-    const int64_t id = tid < a.top ? a.top_ids[row * a.top + tid] : -1;
-    const float t = id >= 0 ? a.top_logits[row * a.top + tid] : -INFINITY;
-    const float tm = over_workgroup(t, part, Max());
-    const float ty = (t - (tm == -INFINITY ? 0.0f : tm)) * a.scale;
-    float q = exp2f(ty * kLog2E);
-    const float mass = over_workgroup(q, part, Sum());
-    const float beyond = over_workgroup(id >= a.classes ? 1.0f : 0.0f, part, Max());
-    const bool taught = a.w_teacher != 0.0f && (mass != 0.0f || beyond != 0.0f);
-    const int64_t label = a.labels ? a.labels[row] : -1;
-    const bool labelled = a.w_label != 0.0f && label >= 0;
-    const float wt = !taught ? 0.0f : beyond != 0.0f || mass != mass ? NAN : a.w_teacher;
-    const float wl = !labelled ? 0.0f : label >= a.classes ? NAN : a.w_label;
-    if (mass != 0.0f) q /= mass;
-    // the student's sums
-    float m = -INFINITY, s1 = 0.0f, st = 0.0f;
+    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes);
+    const int64_t label = a.labels && a.w_label != 0.0f ? a.labels[row] : -1;
+    const int extra = z.beside(tid);
+    if (tid < 64) take_teacher(teacher, a, row, z.z, label);
+    Sums<TWO> o{-INFINITY, 0.0f, 0.0f};
     if (a.given_stats) {
-      m = a.given_stats[row * 3];
-      s1 = a.given_stats[row * 3 + 1];
-      st = a.given_stats[row * 3 + 2];
+      const float* const st = a.given_stats + row * 3;
+      o = Sums<TWO>{st[0], a.w_teacher != 0.0f ? st[2] : st[1], st[1]};
+      __syncthreads();
     } else {
-      for (long long v = tid; v < a.classes; v += kThreads) m = fmaxf(m, as_float(z[v]));
-      m = over_workgroup(m, part, Max());
-      const float from = m == -INFINITY ? 0.0f : m;
-      for (long long v = tid; v < a.classes; v += kThreads) {
-        const float y = as_float(z[v]) - from;
-        s1 += exp2f(y * kLog2E);
-        st += exp2f(y * a.scale * kLog2E);
+      const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
+      for (int at = tid; at < z.chunks; at += kThreads * kUnroll) {
+        uint4 raw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
+        float x[kUnroll * N], most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
+#pragma unroll
+        for (int i = 0; i < kUnroll * N; ++i) most = fmaxf(most, x[i]);
+        o.template take<kUnroll * N>(x, most, c);
       }
-      s1 = over_workgroup(s1, part, Sum());
-      st = over_workgroup(st, part, Sum());
+      o.template take<1>(&x0, x0, c);
+      o = over_workgroup(o, part, c);
       if (a.stats && tid == 0) {
-        a.stats[row * 3] = m;
-        a.stats[row * 3 + 1] = a.w_label != 0.0f ? s1 : NAN;
-        a.stats[row * 3 + 2] = a.w_teacher != 0.0f ? st : NAN;
+        a.stats[row * 3] = o.m;
+        a.stats[row * 3 + 1] = a.w_label == 0.0f ? NAN : TWO ? o.sum1 : o.sum;
+        a.stats[row * 3 + 2] = a.w_teacher == 0.0f ? NAN : o.sum;
       }
     }
-    const bool none = (a.w_label != 0.0f ? s1 : st) == 0.0f || (!taught && !labelled);     // nothing to learn from this row
-    const float zi = id >= 0 && id < a.classes ? as_float(z[id]) : 0.0f;
-    if (a.loss) {
-      float l = taught && q != 0.0f ? wt * q * ((ty - logf(mass)) - ((zi - m) * a.scale - logf(st))) : 0.0f;
-      if (tid == 0 && labelled) l += wl == wl ? wl * (logf(s1) - (as_float(z[label]) - m)) : NAN;
-      l = over_workgroup(l, part, Sum());
-      if (tid == 0) a.loss[row] = none ? 0.0f : beyond != 0.0f && taught ? NAN : l;
+    const float sum1 = TWO ? o.sum1 : o.sum;
+    const bool taught = a.w_teacher != 0.0f && (teacher.mass != 0.0f || teacher.beyond), labelled = label >= 0;
+    const float wt = !taught ? 0.0f : teacher.beyond || teacher.mass != teacher.mass ? NAN : a.w_teacher;
+    const float wl = !labelled ? 0.0f : label >= a.classes ? NAN : a.w_label;
+    const bool none = o.sum == 0.0f || (!taught && !labelled);       // nothing to learn from this row
+    if (a.loss && tid < 64) {
+      const float log_sum = logf(o.sum);
+      float l = 0.0f;
+      for (int k = tid; k < a.top && taught; k += 64)
+        if (teacher.q[k] != 0.0f) l += teacher.q[k] * (teacher.log_q[k] - ((teacher.z[k] - o.m) * a.scale - log_sum));
+#pragma unroll
+      for (int s = 32; s >= 1; s >>= 1) l += __shfl_xor(l, s, 64);
+      l = taught ? l * wt : 0.0f;
+      if (labelled) l += wl * ((TWO ? logf(sum1) : log_sum) - (teacher.z_label - o.m));
+      if (tid == 0) a.loss[row] = none ? 0.0f : l;
     }
-    if (g) {
+    if (a.grad) {
+      T* const g = (T*)a.grad + row * a.grad_stride;
       const float up = a.grad_loss ? a.grad_loss[row] : 1.0f;
       const float ct = up * wt * a.scale, cl = up * wl;
-      __syncthreads();
-      if (tid < a.top) {
-        id_of[tid] = id;
-        mass_of[tid] = q;
-      }
-      __syncthreads();
-      // the classes of the teacher's entries and the label: what one thread for each entry puts there after the others
+      // factors of the exponentials
+      const float k1 = TWO && labelled ? cl / sum1 : 0.0f, kt = (taught ? ct / o.sum : 0.0f) + (!TWO && labelled ? cl / o.sum : 0.0f);
+      const auto slope = [&](float x) {
+        const float y = x - o.m, p = kt * pow2(y * c);
+        return none ? 0.0f : TWO ? fmaf(k1, pow2(y * kLog2E), p) : p;
+      };
+      // what the thread of an entry or of the label puts there at the end
       float mine = 0.0f;
-      const int64_t at = tid < a.top ? id : tid == a.top ? label : -1;
-      if (at >= 0 && at < a.classes && !none) {
-        const float y = as_float(z[at]) - m;
-        mine = (taught ? exp2f(y * a.scale * kLog2E) * (ct / st) : 0.0f) + (labelled ? exp2f(y * kLog2E) * (cl / s1) : 0.0f);
+      const int64_t to = tid < a.top ? teacher.id[tid] : tid == a.top ? label : -1;
+      const bool named = to >= 0 && to < a.classes && !none;
+      if (named) {
         float minus = 0.0f;
-        if (taught)
-          for (int k = 0; k < a.top; ++k) minus += id_of[k] == at ? mass_of[k] : 0.0f;
-        mine -= ct * minus + (labelled && at == label ? cl : 0.0f);
+        for (int k = 0; k < a.top && taught; ++k) minus += teacher.id[k] == to ? teacher.q[k] : 0.0f;
+        mine = slope(tid < a.top ? teacher.z[tid] : teacher.z_label) - ct * minus - (labelled && to == label ? cl : 0.0f);
+      }
+      if (extra >= 0) put(g + extra, slope(as_float(z.z[extra])));
+      const bool same_phase = (((uintptr_t)g ^ (uintptr_t)z.z) & 15) == 0;
+      for (int at = tid; at < z.chunks; at += kThreads * kUnroll) {
+        uint4 raw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          const int ch = at + u * kThreads;
+          if (ch >= z.chunks) break;
+          float x[N];
+          unpack(raw[u], x, (const T*)nullptr);
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[i] = slope(x[i]);
+          T* const out = g + z.head + ch * N;
+          if (same_phase) {
+            *(uint4*)out = pack(x, (const T*)nullptr);
+          } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) put(out + i, x[i]);
+          }
+        }
       }
       __syncthreads();
-      for (long long v = tid; v < a.classes; v += kThreads) {
-        const float y = as_float(z[v]) - m;
-        const float x = (taught ? exp2f(y * a.scale * kLog2E) * (ct / st) : 0.0f) + (labelled ? exp2f(y * kLog2E) * (cl / s1) : 0.0f);
-        put(g + v, none ? 0.0f : x);
-      }
-      __syncthreads();
-      if (at >= 0 && at < a.classes && !none) put(g + at, mine);
+      if (named) put(g + to, mine);
     }
+    __syncthreads();       // (the next row's teacher takes the place of this one's)
   }
 }
 
@@ -439,11 +545,20 @@ int check_grad(const char* who, const void* grad, int32_t dtype, int64_t rows, i
   return CG_OK;
 }
 
+template <class T>
+void launch_distill_of(const DistillArgs& a, hipStream_t s) {
+  const bool two = a.scale != 1.0f && a.w_teacher != 0.0f && a.w_label != 0.0f;
+  if (two)
+    hipLaunchKernelGGL((distill_kernel<T, true>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((distill_kernel<T, false>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+}
+
 int launch_distill(const char* who, const DistillArgs& a, int32_t dtype, hipStream_t s) {
   if (dtype == CG_F32)
-    hipLaunchKernelGGL(distill_kernel<float>, dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+    launch_distill_of<float>(a, s);
   else
-    hipLaunchKernelGGL(distill_kernel<uint16_t>, dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+    launch_distill_of<uint16_t>(a, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return cg::set_error(CG_EHIP, "%s: %s", who, hipGetErrorString(e));
   return CG_OK;
