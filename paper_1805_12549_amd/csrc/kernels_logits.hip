@@ -6,7 +6,7 @@
 // All sums are held in 32 bits.
 #include <hip/hip_runtime.h>
 
-#include <cfloat>
+#include <algorithm>
 #include <cmath>
 
 #include "cg_device.h"
@@ -40,25 +40,31 @@ __device__ __forceinline__ uint64_t rank_key(float z, uint32_t index) {
 // exp2 by the hardware (one ulp; results below 2^-126 are 0)
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A row as the lanes of a workgroup walk it: elements in front of the first 16-byte boundary, whole 16-byte chunks, elements behind the last one.
+// A row as the lanes of a workgroup walk it: elements in front of the first 16-byte boundary, whole 16-byte chunks, elements behind the last one; or
+// part `seg` of `segs` of its chunks, the elements beside them with the first part.
 template <class T>
 struct RowSpan {
   static constexpr int kPer = 16 / (int)sizeof(T);      // elements of a chunk
   const T* z;
   const uint4* body;
-  int head, chunks, tail_from, classes;
-  __device__ RowSpan(const T* row, int n) : z(row), classes(n) {
+  int from, chunks;        // the element at which the part's chunks begin, their number
+  int head, tail_from, end;
+  __device__ RowSpan(const T* row, int n, int seg, int segs) : z(row), end(n) {
     const int lead = (int)((0 - (uintptr_t)row) & 15) / (int)sizeof(T);
     head = lead < n ? lead : n;
-    chunks = (n - head) / kPer;
-    body = (const uint4*)(row + head);
-    tail_from = head + chunks * kPer;
+    const int all = (n - head) / kPer, each = segs == 1 ? all : (all + segs - 1) / segs, first = seg * each;
+    tail_from = head + all * kPer;
+    chunks = first >= all ? 0 : all - first < each ? all - first : each;
+    from = head + first * kPer;
+    body = (const uint4*)(row + from);
+    if (seg) head = 0, tail_from = end;
   }
   // the element beside the chunks that lane `tid` takes (fewer than 16 in all), or -1
   __device__ int beside(int tid) const {
     const int v = tid < head ? tid : tail_from + tid - head;
-    return v < (tid < head ? head : classes) ? v : -1;
+    return v < (tid < head ? head : end) ? v : -1;
   }
+  __device__ bool holds(int64_t v) const { return v < head || (v >= from && v < from + (int64_t)chunks * kPer) || (v >= tail_from && v < end); }
 };
 
 __device__ __forceinline__ void unpack(const uint4& c, float* x, const float*) {
@@ -109,16 +115,19 @@ struct Online {
   }
 };
 
-// over the workgroup; every thread gets the result.  `part`: one value for each wavefront, free again after the next barrier
-__device__ __forceinline__ Online over_workgroup(Online o, Online* part, float c) {
+__device__ __forceinline__ Online from_lane(const Online& o, int mask) {
+  return Online{__shfl_xor(o.m, mask, 64), __shfl_xor(o.sum, mask, 64), __shfl_xor(o.moment, mask, 64)};
+}
+template <class S>
+__device__ __forceinline__ S over_wavefront(S o, float c) {
 #pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) {
-    Online b;
-    b.m = __shfl_xor(o.m, s, 64);
-    b.sum = __shfl_xor(o.sum, s, 64);
-    b.moment = __shfl_xor(o.moment, s, 64);
-    o.join(b, c);
-  }
+  for (int s = 32; s >= 1; s >>= 1) o.join(from_lane(o, s), c);
+  return o;
+}
+// every thread gets the result.  `part`: one value for each wavefront, free again after the next barrier
+template <class S>
+__device__ __forceinline__ S over_workgroup(S o, S* part, float c) {
+  o = over_wavefront(o, c);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = o;
   __syncthreads();
@@ -183,26 +192,54 @@ __device__ __forceinline__ void add_found(TopLds& l, uint64_t key) {
 struct LogprobArgs {
   const void* logits;
   long long rows, stride;
-  int classes, given, top;
+  int classes, given, top, segs;
   float scale;             // 1 / temperature
   const int64_t* labels;
   float *logprob, *entropy;
   int64_t* top_ids;
   float* top_logprobs;
+  Online* parts;           // [rows][segs] and their greatest keys [rows][segs][top] (0: fewer than that), where rows are shared out
+  uint64_t* keys;
+};
+
+__device__ __forceinline__ void put_top(const LogprobArgs& a, long long row, int at, int64_t id, float logprob) {
+  a.top_ids[row * a.top + at] = id;
+  a.top_logprobs[row * a.top + at] = logprob;
+}
+
+// What a row's sums give, and how its log probabilities come from them.
+template <class T>
+struct RowAnswer {
+  const T* z;
+  float m, scale, log_sum;
+  bool none, bad;
+  __device__ RowAnswer(const LogprobArgs& a, long long row, const Online& o)
+      : z((const T*)a.logits + row * a.stride), m(o.m), scale(a.scale), log_sum(logf(o.sum)), none(o.sum == 0.0f), bad(o.sum != o.sum) {
+    const int tid = (int)threadIdx.x;
+    for (int g = tid; g < a.given; g += kThreads) {
+      const int64_t id = a.labels[row * a.given + g];
+      a.logprob[row * a.given + g] = id < 0 ? 0.0f : id >= a.classes ? NAN : of((uint32_t)id);
+    }
+    if (a.entropy && tid == 0) a.entropy[row] = none ? 0.0f : log_sum - o.moment / (o.sum * kLog2E);
+    if (bad && tid < a.top) put_top(a, row, tid, -1, NAN);
+  }
+  __device__ float of(uint32_t id) const { return none ? -INFINITY : bad ? NAN : (as_float(z[id]) - m) * scale - log_sum; }
 };
 
 // One pass over the row (V elements are read once): every lane keeps its own running maximum and sums.  The alternatives come from what the pass
 // leaves behind: the lanes' maxima give a bound that is reached by little more than `top` classes, the maxima of each lane's stretches say where those
-// lie, and only such stretches are read again.
-template <class T>
+// lie, and only such stretches are read again.  PART: a workgroup takes one of `segs` parts of a row, and leaves its sums and keys to
+// logprobs_join_kernel.
+template <class T, bool PART>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
   __shared__ Online part[kWaves];
   __shared__ TopLds top;
   constexpr int N = RowSpan<T>::kPer;
-  const int tid = (int)threadIdx.x;
+  const int tid = (int)threadIdx.x, segs = PART ? a.segs : 1;
   const float c = a.scale * kLog2E;
-  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes);
+  for (long long i = blockIdx.x; i < a.rows * segs; i += gridDim.x) {
+    const long long row = PART ? i / segs : i;
+    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes, PART ? (int)(i - row * segs) : 0, segs);
     const int groups = (z.chunks + kThreads * kUnroll - 1) / (kThreads * kUnroll);
     const int per_mark = (groups + kMarks - 1) / kMarks;       // groups of a stretch
     const int extra = z.beside(tid);
@@ -218,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
 #pragma unroll
-      for (int i = 0; i < kUnroll * N; ++i) most = fmaxf(most, x[i]);
+      for (int e = 0; e < kUnroll * N; ++e) most = fmaxf(most, x[e]);
       o.take<kUnroll * N>(x, most, c);
       stretch = fmaxf(stretch, most);
       if (++in == per_mark || g + 1 == groups) {
@@ -229,49 +266,81 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
       }
     }
     o.take<1>(&x0, x0, c);
-    const bool holds = tid < z.chunks || extra >= 0;
-    const uint64_t mine = holds ? rank_key(o.m, ~0u) : 0;
+    const uint64_t mine = tid < z.chunks || extra >= 0 ? rank_key(o.m, ~0u) : 0;
     o = over_workgroup(o, part, c);
-    const bool none = o.sum == 0.0f, bad = o.sum != o.sum;
-    const float log_sum = logf(o.sum);
-    const auto logprob = [&](float x) { return none ? -INFINITY : bad ? NAN : (x - o.m) * a.scale - log_sum; };
-    for (int g = tid; g < a.given; g += kThreads) {
-      const int64_t id = a.labels[row * a.given + g];
-      a.logprob[row * a.given + g] = id < 0 ? 0.0f : id >= a.classes ? NAN : logprob(as_float(z.z[id]));
-    }
-    if (a.entropy && tid == 0) a.entropy[row] = none ? 0.0f : log_sum - o.moment / (o.sum * kLog2E);
-    if (!a.top) continue;
-    if (bad) {
-      if (tid < a.top) {
-        a.top_ids[row * a.top + tid] = -1;
-        a.top_logprobs[row * a.top + tid] = NAN;
-      }
-      continue;
-    }
-    const int n = find_top(top, mine, a.top, [&](uint64_t bound) {
-      const auto offer = [&](float x, int v) {
-        const uint64_t key = rank_key(x, (uint32_t)v);
-        if (key >= bound) add_found(top, key);
-      };
-      if (extra >= 0) offer(x0, extra);
-      for (int mark = 0; mark * per_mark < groups; ++mark) {
-        if (rank_key(top.mark[mark][tid], 0) < bound) continue;
-        const int g1 = (mark + 1) * per_mark < groups ? (mark + 1) * per_mark : groups;
-        for (int ch = mark * per_mark * kThreads * kUnroll + tid; ch < g1 * kThreads * kUnroll && ch < z.chunks; ch += kThreads) {
-          float x[N];
-          unpack(z.body[ch], x, (const T*)nullptr);
+    const bool bad = o.sum != o.sum;
+    const auto find = [&]() {
+      return find_top(top, mine, a.top, [&](uint64_t bound) {
+        const auto offer = [&](float x, int v) {
+          const uint64_t key = rank_key(x, (uint32_t)v);
+          if (key >= bound) add_found(top, key);
+        };
+        if (extra >= 0) offer(x0, extra);
+        for (int mark = 0; mark * per_mark < groups; ++mark) {
+          if (rank_key(top.mark[mark][tid], 0) < bound) continue;
+          const int g1 = (mark + 1) * per_mark < groups ? (mark + 1) * per_mark : groups;
+          for (int ch = mark * per_mark * kThreads * kUnroll + tid; ch < g1 * kThreads * kUnroll && ch < z.chunks; ch += kThreads) {
+            float x[N];
+            unpack(z.body[ch], x, (const T*)nullptr);
 #pragma unroll
-          for (int i = 0; i < N; ++i) offer(x[i], z.head + ch * N + i);
+            for (int e = 0; e < N; ++e) offer(x[e], z.from + ch * N + e);
+          }
         }
+      });
+    };
+    if (PART) {
+      if (tid == 0) a.parts[i] = o;
+      if (!a.top) continue;
+      const int n = bad ? 0 : find();
+      uint64_t* const keys = a.keys + i * a.top;
+      for (int k = tid; k < n; k += kThreads) {
+        const int r = rank_among(top.found, n, top.found[k], k);
+        if (r < a.top) keys[r] = top.found[k];
       }
+      for (int k = n + tid; k < a.top; k += kThreads) keys[k] = 0;
+    } else {
+      const RowAnswer<T> answer(a, row, o);
+      if (!a.top || bad) continue;
+      const int n = find();
+      for (int k = tid; k < n; k += kThreads) {
+        const uint32_t id = ~(uint32_t)top.found[k];
+        const int r = rank_among(top.found, n, top.found[k], k);
+        if (r < a.top) put_top(a, row, r, id, answer.of(id));
+      }
+    }
+  }
+}
+
+// parts[0, n), joined by each wavefront by itself
+template <class S>
+__device__ __forceinline__ S join_parts(const S* parts, int n, S o, float c) {
+  for (int k = (int)threadIdx.x & 63; k < n; k += 64) o.join(parts[k], c);
+  o = over_wavefront(o, c);
+  S one = o;                     // (the first lane's: the lanes' own may differ by a rounding)
+  uint32_t* const w = (uint32_t*)&one;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(S) / 4); ++i) w[i] = __builtin_amdgcn_readfirstlane(((const uint32_t*)&o)[i]);
+  return one;
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) {
+  __shared__ TopLds top;
+  const int tid = (int)threadIdx.x, n_keys = a.segs * a.top;
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const uint64_t* const keys = a.keys + row * n_keys;
+    uint64_t mine = 0;
+    for (int k = tid; k < n_keys; k += kThreads) mine = keys[k] > mine ? keys[k] : mine;
+    const RowAnswer<T> answer(a, row, join_parts(a.parts + row * a.segs, a.segs, Online{-INFINITY, 0.0f, 0.0f}, a.scale * kLog2E));
+    if (!a.top || answer.bad) continue;
+    const int n = find_top(top, mine, a.top, [&](uint64_t bound) {
+      for (int k = tid; k < n_keys; k += kThreads)
+        if (keys[k] && keys[k] >= bound) add_found(top, keys[k]);
     });
-    for (int i = tid; i < n; i += kThreads) {
-      const uint64_t key = top.found[i];
-      const int r = rank_among(top.found, n, key, i);
-      if (r >= a.top) continue;
-      const uint32_t id = ~(uint32_t)key;
-      a.top_ids[row * a.top + r] = (int64_t)id;
-      a.top_logprobs[row * a.top + r] = logprob(as_float(z.z[id]));
+    for (int k = tid; k < n; k += kThreads) {
+      const uint32_t id = ~(uint32_t)top.found[k];
+      const int r = rank_among(top.found, n, top.found[k], k);
+      if (r < a.top) put_top(a, row, r, id, answer.of(id));
     }
   }
 }
@@ -289,6 +358,8 @@ struct DistillArgs {
   const float* given_stats;
   float *loss, *stats;
   void* grad;
+  int segs, n_parts;       // parts of a row that this launch works on, and that the launch before it did (0: none)
+  float* parts;            // [rows][parts][3]
 };
 
 // The teacher's side of a row and the logits that its terms ask for, taken by the first wavefront while the others start on the row.
@@ -370,22 +441,8 @@ struct Sums {
   }
 };
 template <bool TWO>
-__device__ __forceinline__ Sums<TWO> over_workgroup(Sums<TWO> o, Sums<TWO>* part, float c) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) {
-    Sums<TWO> b;
-    b.m = __shfl_xor(o.m, s, 64);
-    b.sum = __shfl_xor(o.sum, s, 64);
-    b.sum1 = TWO ? __shfl_xor(o.sum1, s, 64) : 0.0f;
-    o.join(b, c);
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = o;
-  __syncthreads();
-  o = part[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) o.join(part[w], c);
-  return o;
+__device__ __forceinline__ Sums<TWO> from_lane(const Sums<TWO>& o, int mask) {
+  return Sums<TWO>{__shfl_xor(o.m, mask, 64), __shfl_xor(o.sum, mask, 64), TWO ? __shfl_xor(o.sum1, mask, 64) : 0.0f};
 }
 
 __device__ __forceinline__ uint4 pack(const float* g, const float*) {
@@ -398,7 +455,43 @@ __device__ __forceinline__ uint4 pack(const float* g, const uint16_t*) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Loss and gradient of a row.  One pass for the sums (none where the call brings them), one that writes the gradient: for every class the
+// The exponentials' factor of the first sum (the only one, or the teacher's).
+__device__ __forceinline__ float first_factor(const DistillArgs& a) { return a.w_teacher != 0.0f ? a.scale * kLog2E : kLog2E; }
+
+template <class T, bool TWO>
+__device__ __forceinline__ Sums<TWO> sums_of(const RowSpan<T>& z, int extra, float c, Sums<TWO>* part) {
+  constexpr int N = RowSpan<T>::kPer;
+  Sums<TWO> o{-INFINITY, 0.0f, 0.0f};
+  const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
+  for (int at = (int)threadIdx.x; at < z.chunks; at += kThreads * kUnroll) {
+    uint4 raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
+    float x[kUnroll * N], most = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
+#pragma unroll
+    for (int i = 0; i < kUnroll * N; ++i) most = fmaxf(most, x[i]);
+    o.template take<kUnroll * N>(x, most, c);
+  }
+  o.template take<1>(&x0, x0, c);
+  return over_workgroup(o, part, c);
+}
+
+// the sums of parts of rows, where rows are shared out
+template <class T, bool TWO>
+__global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs a) {
+  __shared__ Sums<TWO> part[kWaves];
+  for (long long i = blockIdx.x; i < a.rows * a.segs; i += gridDim.x) {
+    const long long row = i / a.segs;
+    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes, (int)(i - row * a.segs), a.segs);
+    const Sums<TWO> o = sums_of<T, TWO>(z, z.beside((int)threadIdx.x), first_factor(a), part);
+    if (threadIdx.x == 0) ((Sums<TWO>*)a.parts)[i] = o;
+  }
+}
+
+// Loss and gradient of a row, or of one of `segs` parts of it.  One pass for the sums (none where the call brings them, or where a launch before
+// has formed those of parts), one that writes the gradient: for every class the
 // probabilities' part; then the classes that the label or the teacher names are written again, in full and rounded once.  TWO: both terms
 // are there at different temperatures, that is two sums and two exponentials an element.
 template <class T, bool TWO>
@@ -407,9 +500,11 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
   __shared__ TeacherLds teacher;
   constexpr int N = RowSpan<T>::kPer;
   const int tid = (int)threadIdx.x;
-  const float c = a.w_teacher != 0.0f ? a.scale * kLog2E : kLog2E;
-  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes);
+  const float c = first_factor(a);
+  for (long long i = blockIdx.x; i < a.rows * a.segs; i += gridDim.x) {
+    const long long row = i / a.segs;
+    const int seg = (int)(i - row * a.segs);
+    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes, seg, a.segs);
     const int64_t label = a.labels && a.w_label != 0.0f ? a.labels[row] : -1;
     const int extra = z.beside(tid);
     if (tid < 64) take_teacher(teacher, a, row, z.z, label);
@@ -418,33 +513,23 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
       const float* const st = a.given_stats + row * 3;
       o = Sums<TWO>{st[0], a.w_teacher != 0.0f ? st[2] : st[1], st[1]};
       __syncthreads();
+    } else if (a.n_parts) {
+      o = join_parts((const Sums<TWO>*)a.parts + row * a.n_parts, a.n_parts, o, c);
+      __syncthreads();
     } else {
-      const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
-      for (int at = tid; at < z.chunks; at += kThreads * kUnroll) {
-        uint4 raw[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
-        float x[kUnroll * N], most = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
-#pragma unroll
-        for (int i = 0; i < kUnroll * N; ++i) most = fmaxf(most, x[i]);
-        o.template take<kUnroll * N>(x, most, c);
-      }
-      o.template take<1>(&x0, x0, c);
-      o = over_workgroup(o, part, c);
-      if (a.stats && tid == 0) {
-        a.stats[row * 3] = o.m;
-        a.stats[row * 3 + 1] = a.w_label == 0.0f ? NAN : TWO ? o.sum1 : o.sum;
-        a.stats[row * 3 + 2] = a.w_teacher == 0.0f ? NAN : o.sum;
-      }
+      o = sums_of<T, TWO>(z, extra, c, part);
+    }
+    if (a.stats && seg == 0 && tid == 0) {
+      a.stats[row * 3] = o.m;
+      a.stats[row * 3 + 1] = a.w_label == 0.0f ? NAN : TWO ? o.sum1 : o.sum;
+      a.stats[row * 3 + 2] = a.w_teacher == 0.0f ? NAN : o.sum;
     }
     const float sum1 = TWO ? o.sum1 : o.sum;
     const bool taught = a.w_teacher != 0.0f && (teacher.mass != 0.0f || teacher.beyond), labelled = label >= 0;
     const float wt = !taught ? 0.0f : teacher.beyond || teacher.mass != teacher.mass ? NAN : a.w_teacher;
     const float wl = !labelled ? 0.0f : label >= a.classes ? NAN : a.w_label;
     const bool none = o.sum == 0.0f || (!taught && !labelled);       // nothing to learn from this row
-    if (a.loss && tid < 64) {
+    if (a.loss && seg == 0 && tid < 64) {
       const float log_sum = logf(o.sum);
       float l = 0.0f;
       for (int k = tid; k < a.top && taught; k += 64)
@@ -468,7 +553,7 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
       // what the thread of an entry or of the label puts there at the end
       float mine = 0.0f;
       const int64_t to = tid < a.top ? teacher.id[tid] : tid == a.top ? label : -1;
-      const bool named = to >= 0 && to < a.classes && !none;
+      const bool named = to >= 0 && !none && z.holds(to);
       if (named) {
         float minus = 0.0f;
         for (int k = 0; k < a.top && taught; ++k) minus += teacher.id[k] == to ? teacher.q[k] : 0.0f;
@@ -488,7 +573,7 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
           unpack(raw[u], x, (const T*)nullptr);
 #pragma unroll
           for (int i = 0; i < N; ++i) x[i] = slope(x[i]);
-          T* const out = g + z.head + ch * N;
+          T* const out = g + z.from + ch * N;
           if (same_phase) {
             *(uint4*)out = pack(x, (const T*)nullptr);
           } else {
@@ -545,13 +630,48 @@ int check_grad(const char* who, const void* grad, int32_t dtype, int64_t rows, i
   return CG_OK;
 }
 
+// Parts of a row: where there are few rows, as many as give a launch kEnough workgroups, each with kUnroll chunks for a lane at least.
+constexpr int kEnough = 512;
+int parts_of(int64_t rows, int64_t classes, int bytes) {
+  if (rows <= 0 || rows >= kEnough) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>((kEnough + rows - 1) / rows, classes * bytes / (kThreads * kUnroll * 16)));
+}
+
+template <class T>
+void launch_logprobs(const LogprobArgs& a, hipStream_t s) {
+  if (a.segs > 1) {
+    hipLaunchKernelGGL((logprobs_kernel<T, true>), dim3((unsigned)(a.rows * a.segs)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((logprobs_kernel<T, false>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+  }
+}
+
+template <class T, bool TWO>
+void launch_distill_as(DistillArgs a, hipStream_t s) {
+  const int segs = parts_of(a.rows, a.classes, sizeof(T));
+  a.segs = segs;
+  if (segs > 1 && !a.given_stats) {
+    hipLaunchKernelGGL((distill_part_kernel<T, TWO>), dim3((unsigned)(a.rows * segs)), dim3(kThreads), 0, s, a);
+    a.n_parts = segs;
+    if (a.grad == a.logits) {      // the loss asks for logits that another part's workgroup replaces by their gradient: it goes first
+      DistillArgs first = a;
+      first.grad = nullptr;
+      first.segs = 1;
+      hipLaunchKernelGGL((distill_kernel<T, TWO>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, first);
+      a.loss = nullptr;
+    }
+    if (!a.grad) a.segs = 1;
+  }
+  hipLaunchKernelGGL((distill_kernel<T, TWO>), dim3(row_groups(a.rows * a.segs)), dim3(kThreads), 0, s, a);
+}
+
 template <class T>
 void launch_distill_of(const DistillArgs& a, hipStream_t s) {
-  const bool two = a.scale != 1.0f && a.w_teacher != 0.0f && a.w_label != 0.0f;
-  if (two)
-    hipLaunchKernelGGL((distill_kernel<T, true>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+  if (a.scale != 1.0f && a.w_teacher != 0.0f && a.w_label != 0.0f)
+    launch_distill_as<T, true>(a, s);
   else
-    hipLaunchKernelGGL((distill_kernel<T, false>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+    launch_distill_as<T, false>(a, s);
 }
 
 int launch_distill(const char* who, const DistillArgs& a, int32_t dtype, hipStream_t s) {
@@ -569,8 +689,10 @@ int launch_distill(const char* who, const DistillArgs& a, int32_t dtype, hipStre
 extern "C" {
 
 size_t cg_logprobs_workspace_bytes(int64_t rows, int32_t classes, int32_t top) {
-  (void)rows, (void)classes, (void)top;
-  return 0;
+  if (rows <= 0 || classes <= 0 || top < 0 || top > CG_TOP_MAX) return 0;
+  // (the larger of the two types' needs)
+  const int segs = parts_of(rows, classes, 4);
+  return segs == 1 ? 0 : (size_t)rows * segs * (sizeof(Online) + 8 + 8 * (size_t)top);
 }
 
 int cg_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t classes, int64_t row_stride, float temperature, const int64_t* labels,
@@ -588,19 +710,25 @@ int cg_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t classes
   const size_t need = cg_logprobs_workspace_bytes(rows, classes, top);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256)))
     return cg::set_error(CG_EINVAL, "%s: needs %zu bytes of workspace, 256-byte aligned", who, need);
-  const LogprobArgs a{logits, rows, row_stride, classes, given, top, 1.0f / temperature, labels, logprob, entropy, top_ids, top_logprobs};
+  LogprobArgs a{logits, rows, row_stride, classes, given, top, 1, 1.0f / temperature, labels, logprob, entropy, top_ids, top_logprobs, nullptr, nullptr};
+  a.segs = parts_of(rows, classes, element_bytes(dtype));
+  if (a.segs > 1) {
+    a.keys = (uint64_t*)workspace;
+    a.parts = (Online*)(a.keys + rows * a.segs * top);
+  }
   if (dtype == CG_F32)
-    hipLaunchKernelGGL(logprobs_kernel<float>, dim3(row_groups(rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    launch_logprobs<float>(a, (hipStream_t)hip_stream);
   else
-    hipLaunchKernelGGL(logprobs_kernel<uint16_t>, dim3(row_groups(rows)), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    launch_logprobs<uint16_t>(a, (hipStream_t)hip_stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return cg::set_error(CG_EHIP, "%s: %s", who, hipGetErrorString(e));
   return CG_OK;
 }
 
 size_t cg_distill_workspace_bytes(int64_t rows, int32_t classes) {
-  (void)rows, (void)classes;
-  return 0;
+  if (rows <= 0 || classes <= 0) return 0;
+  const int segs = parts_of(rows, classes, 4);      // (the larger of the two types' needs)
+  return segs == 1 ? 0 : (size_t)rows * segs * 3 * sizeof(float);
 }
 
 int cg_distill_forward(const void* logits, int32_t dtype, int64_t rows, int32_t classes, int64_t row_stride, float temperature, const int64_t* top_ids,
@@ -619,7 +747,7 @@ int cg_distill_forward(const void* logits, int32_t dtype, int64_t rows, int32_t 
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256)))
     return cg::set_error(CG_EINVAL, "%s: needs %zu bytes of workspace, 256-byte aligned", who, need);
   const DistillArgs a{logits, rows, row_stride, grad_stride, classes, top, 1.0f / temperature, teacher_weight, label_weight, top_ids, top_logits,
-                      labels, grad_loss, nullptr, loss, stats, grad};
+                      labels, grad_loss, nullptr, loss, stats, grad, 1, 0, (float*)workspace};
   return launch_distill(who, a, dtype, (hipStream_t)hip_stream);
 }
 
@@ -634,7 +762,7 @@ int cg_distill_backward(const void* logits, int32_t dtype, int64_t rows, int32_t
   if (const int rc = check_grad(who, grad, dtype, rows, classes, grad_stride, logits, row_stride)) return rc;
   if (rows == 0) return CG_OK;
   const DistillArgs a{logits, rows, row_stride, grad_stride, classes, top, 1.0f / temperature, teacher_weight, label_weight, top_ids, top_logits,
-                      labels, grad_loss, stats, nullptr, nullptr, grad};
+                      labels, grad_loss, stats, nullptr, nullptr, grad, 1, 0, nullptr};
   return launch_distill(who, a, dtype, (hipStream_t)hip_stream);
 }
 
