@@ -83,6 +83,28 @@ __device__ __forceinline__ uint4 all_minus_inf() {
 
 constexpr float kLeast = -1.0e4f;     // in the place of exponents from there down to -inf, whose power is 0, where they are factors of it
 
+// Over a wavefront whose lanes are all active: across the lanes of a row of 16 by moves between neighbours, then the four rows' results, which are
+// the same bits in every lane.  (A shuffle through LDS takes some hundred clocks, a move a few.)
+template <int kMove>
+__device__ __forceinline__ float moved(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), kMove, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_of(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
+template <class Op>
+__device__ __forceinline__ float over_lanes(float x, Op op) {
+  x = op(x, moved<0xB1>(x));       // the other of a pair
+  x = op(x, moved<0x4E>(x));       // the other pair of four
+  x = op(x, moved<0x141>(x));      // mirrored in eight
+  x = op(x, moved<0x140>(x));      // mirrored in sixteen
+  return op(op(lane_of(x, 0), lane_of(x, 16)), op(lane_of(x, 32), lane_of(x, 48)));
+}
+__device__ __forceinline__ float max_over_lanes(float x) {
+  return over_lanes(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float sum_over_lanes(float x) {
+  return over_lanes(x, [](float a, float b) { return a + b; });
+}
+
 // A softmax in one pass: with m the greatest logit so far, the sum of e = 2^((z - m) c) and the sum of e (z - m) c, c = log2(e) / temperature.
 // A new maximum scales both.  NaN and +inf make the sum NaN; without any class m is -inf and the sum 0.
 struct Online {
@@ -105,36 +127,45 @@ struct Online {
       moment = fmaf(e, fmaxf(y, kLeast), moment);
     }
   }
-  __device__ void join(const Online& o, float c) {
-    Online b = o;
-    const float to = fmaxf(m, b.m);
-    raise(to, c);
-    b.raise(to, c);
+  __device__ void add(const Online& b) {
     sum += b.sum;
     moment += b.moment;
   }
+  __device__ void over_lanes() {
+    sum = sum_over_lanes(sum);
+    moment = sum_over_lanes(moment);
+  }
 };
 
-__device__ __forceinline__ Online from_lane(const Online& o, int mask) {
-  return Online{__shfl_xor(o.m, mask, 64), __shfl_xor(o.sum, mask, 64), __shfl_xor(o.moment, mask, 64)};
+template <class S>
+__device__ __forceinline__ void join(S& o, S b, float c) {
+  const float to = fmaxf(o.m, b.m);
+  o.raise(to, c);
+  b.raise(to, c);
+  o.add(b);
 }
 template <class S>
 __device__ __forceinline__ S over_wavefront(S o, float c) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) o.join(from_lane(o, s), c);
+  o.raise(max_over_lanes(o.m), c);
+  o.over_lanes();
   return o;
 }
-// every thread gets the result.  `part`: one value for each wavefront, free again after the next barrier
+// Every thread gets the result.  `part`: one value for each wavefront, not those of the row before.
 template <class S>
 __device__ __forceinline__ S over_workgroup(S o, S* part, float c) {
   o = over_wavefront(o, c);
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = o;
   __syncthreads();
   o = part[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) o.join(part[w], c);
+  for (int w = 1; w < kWaves; ++w) join(o, part[w], c);
   return o;
+}
+// parts[0, n), joined by each wavefront by itself
+template <class S>
+__device__ __forceinline__ S join_parts(const S* parts, int n, S o, float c) {
+  for (int k = (int)threadIdx.x & 63; k < n; k += 64) join(o, parts[k], c);
+  return over_wavefront(o, c);
 }
 
 constexpr int kUnroll = 4;           // chunks that a lane has on their way
@@ -143,51 +174,71 @@ constexpr int kCandidates = 1024;    // at most so many are compared with each o
 
 struct TopLds {
   float mark[kMarks][kThreads];      // of each lane's stretches
-  alignas(16) uint64_t lane_key[kThreads];
+  uint32_t lane[2][kThreads];        // upper halves of the lanes' greatest keys (0: none), for rows in turn
+  int count[2];
   alignas(16) uint64_t found[kCandidates];
   uint64_t bound;
-  int count;
 };
 
-// how many of keys[0, n) come before `key`, the entry `at`
-__device__ __forceinline__ int rank_among(const uint64_t* keys, int n, uint64_t key, int at) {
-  int r = 0;
-  int j = 0;
+// how many of keys[0, n), all different, are greater than `key`
+__device__ __forceinline__ int rank_among(const uint64_t* keys, int n, uint64_t key) {
+  int r = 0, j = 0;
+#pragma unroll 4
   for (; j + 2 <= n; j += 2) {
     const ulonglong2 k = *(const ulonglong2*)(keys + j);
-    r += (k.x > key || (k.x == key && j < at)) + (k.y > key || (k.y == key && j + 1 < at));
+    r += (k.x > key) + (k.y > key);
   }
-  if (j < n) r += keys[j] > key || (keys[j] == key && j < at);
-  return r;
+  return j < n ? r + (keys[j] > key) : r;
 }
 
-// The `top` greatest keys of a workgroup's lanes: found[0, n) holds them, and few others.  `mine` is not above the greatest key of this lane (0: it
-// has none), scan(bound) puts every key of this lane from `bound` up into `found`.  The top-th of the lanes' own is a bound that at least
-// `top` keys reach; as a rule few more do.  Where `found` does not hold them (equal logits, or a lane that has many of the greatest), the
-// top-th of those that it took, whichever these are, is a higher bound that `top` keys reach, and at least kCandidates - top keys lie below it.
+// What a lane leaves for find_top, before a barrier.
+__device__ __forceinline__ void offer_lane(TopLds& l, int turn, uint32_t upper) {
+  l.lane[turn][threadIdx.x] = upper;
+  if (threadIdx.x == 0) l.count[turn] = 0;
+}
+
+// The `top` greatest keys of a workgroup's lanes, which are all different: found[0, n) holds them, and few others.  scan(bound, add) calls add(key) for
+// every key of this lane from `bound` up.  The top-th of the lanes' greatest, cut to 16 bits, is a bound that at least `top` keys reach; as a
+// rule few more do.  Where `found` does not hold them (equal logits, or a lane that has many of the greatest), the top-th of those
+// that it took, whichever these are, is a higher bound that `top` keys reach, and at least kCandidates - top keys lie below it.
 template <class Scan>
-__device__ int find_top(TopLds& l, uint64_t mine, int top, Scan scan) {
+__device__ int find_top(TopLds& l, int turn, int top, Scan scan) {
   const int tid = (int)threadIdx.x;
-  __syncthreads();
-  l.lane_key[tid] = mine;
-  __syncthreads();
-  if (rank_among(l.lane_key, kThreads, mine, tid) == top - 1) l.bound = mine;
+  uint32_t k[kWaves], cut = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) k[w] = l.lane[turn][w * 64 + (tid & 63)] >> 16;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {       // every wavefront by itself: bit by bit, as long as `top` lanes reach the number
+    const uint32_t next = cut | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(k[w] >= next));
+    cut = n >= top ? next : cut;
+  }
+  uint64_t bound = (uint64_t)cut << 48;
   for (;;) {
-    if (tid == 0) l.count = 0;
+    scan(bound, [&](uint64_t key) {
+      const int at = atomicAdd(&l.count[turn], 1);
+      if (at < kCandidates) l.found[at] = key;
+    });
     __syncthreads();
-    scan(l.bound);
-    __syncthreads();
-    const int n = l.count;
+    const int n = l.count[turn];
     if (n <= kCandidates) return n;
     for (int i = tid; i < kCandidates; i += kThreads)
-      if (rank_among(l.found, kCandidates, l.found[i], i) == top - 1) l.bound = l.found[i];
+      if (rank_among(l.found, kCandidates, l.found[i]) == top - 1) l.bound = l.found[i];
+    __syncthreads();
+    bound = l.bound;
+    if (tid == 0) l.count[turn] = 0;
     __syncthreads();
   }
 }
-__device__ __forceinline__ void add_found(TopLds& l, uint64_t key) {
-  const int at = atomicAdd(&l.count, 1);
-  if (at < kCandidates) l.found[at] = key;
+// the logit of a key
+__device__ __forceinline__ float logit_of(uint64_t key) {
+  const uint32_t up = (uint32_t)(key >> 32);
+  return __uint_as_float(up & 0x80000000u ? up ^ 0x80000000u : ~up);
 }
+// the least logit whose keys may reach the bound (below -inf's own there is none)
+__device__ __forceinline__ float least_logit(uint64_t bound) { return (bound >> 32) < 0x00800000u ? -INFINITY : logit_of(bound); }
 
 struct LogprobArgs {
   const void* logits;
@@ -202,28 +253,44 @@ struct LogprobArgs {
   uint64_t* keys;
 };
 
-__device__ __forceinline__ void put_top(const LogprobArgs& a, long long row, int at, int64_t id, float logprob) {
-  a.top_ids[row * a.top + at] = id;
-  a.top_logprobs[row * a.top + at] = logprob;
-}
-
-// What a row's sums give, and how its log probabilities come from them.
+// A row's log probabilities.  The logits of given classes are on their way while the row is read.
 template <class T>
 struct RowAnswer {
+  const LogprobArgs& a;
   const T* z;
-  float m, scale, log_sum;
+  long long row;
+  int64_t id0;
+  float z0;
+  float m, log_sum;
   bool none, bad;
-  __device__ RowAnswer(const LogprobArgs& a, long long row, const Online& o)
-      : z((const T*)a.logits + row * a.stride), m(o.m), scale(a.scale), log_sum(logf(o.sum)), none(o.sum == 0.0f), bad(o.sum != o.sum) {
+  __device__ RowAnswer(const LogprobArgs& args, long long r) : a(args), z((const T*)args.logits + r * args.stride), row(r) {
+    if ((int)threadIdx.x < a.given) take((int)threadIdx.x);
+  }
+  __device__ void take(int g) {
+    id0 = a.labels[row * a.given + g];
+    z0 = id0 >= 0 && id0 < a.classes ? as_float(z[id0]) : 0.0f;
+  }
+  __device__ void put(const Online& o) {
+    m = o.m, log_sum = logf(o.sum), none = o.sum == 0.0f, bad = o.sum != o.sum;
     const int tid = (int)threadIdx.x;
     for (int g = tid; g < a.given; g += kThreads) {
-      const int64_t id = a.labels[row * a.given + g];
-      a.logprob[row * a.given + g] = id < 0 ? 0.0f : id >= a.classes ? NAN : of((uint32_t)id);
+      if (g != tid) take(g);
+      a.logprob[row * a.given + g] = id0 < 0 ? 0.0f : id0 >= a.classes ? NAN : of(z0);
     }
     if (a.entropy && tid == 0) a.entropy[row] = none ? 0.0f : log_sum - o.moment / (o.sum * kLog2E);
-    if (bad && tid < a.top) put_top(a, row, tid, -1, NAN);
+    if (bad && tid < a.top) put_top(tid, -1, NAN);
   }
-  __device__ float of(uint32_t id) const { return none ? -INFINITY : bad ? NAN : (as_float(z[id]) - m) * scale - log_sum; }
+  __device__ float of(float x) const { return none ? -INFINITY : bad ? NAN : (x - m) * a.scale - log_sum; }
+  __device__ void put_top(int at, int64_t id, float logprob) const {
+    a.top_ids[row * a.top + at] = id;
+    a.top_logprobs[row * a.top + at] = logprob;
+  }
+  __device__ void put_top(const uint64_t* found, int n) const {
+    for (int k = (int)threadIdx.x; k < n; k += kThreads) {
+      const int r = rank_among(found, n, found[k]);
+      if (r < a.top) put_top(r, ~(uint32_t)found[k], of(logit_of(found[k])));
+    }
+  }
 };
 
 // One pass over the row (V elements are read once): every lane keeps its own running maximum and sums.  The alternatives come from what the pass
@@ -232,25 +299,29 @@ struct RowAnswer {
 // logprobs_join_kernel.
 template <class T, bool PART>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
-  __shared__ Online part[kWaves];
+  __shared__ Online part[2][kWaves];
   __shared__ TopLds top;
   constexpr int N = RowSpan<T>::kPer;
   const int tid = (int)threadIdx.x, segs = PART ? a.segs : 1;
   const float c = a.scale * kLog2E;
-  for (long long i = blockIdx.x; i < a.rows * segs; i += gridDim.x) {
+  int turn = 0;
+  for (long long i = blockIdx.x; i < a.rows * segs; i += gridDim.x, turn ^= 1) {
     const long long row = PART ? i / segs : i;
-    const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes, PART ? (int)(i - row * segs) : 0, segs);
+    RowAnswer<T> answer(a, row);
+    const RowSpan<T> z(answer.z, a.classes, PART ? (int)(i - row * segs) : 0, segs);
     const int groups = (z.chunks + kThreads * kUnroll - 1) / (kThreads * kUnroll);
     const int per_mark = (groups + kMarks - 1) / kMarks;       // groups of a stretch
     const int extra = z.beside(tid);
     Online o{-INFINITY, 0.0f, 0.0f};
     const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
     float stretch = -INFINITY;
-    for (int g = 0, in = 0, mark = 0; g < groups; ++g) {
-      uint4 raw[kUnroll];
-      const int at = g * kThreads * kUnroll + tid;
+    uint4 raw[kUnroll];
+    const auto load = [&](int at) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
+    };
+    for (int g = 0, in = 0, mark = 0; g < groups; ++g) {
+      load(g * kThreads * kUnroll + tid);
       float x[kUnroll * N], most = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
@@ -266,24 +337,29 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
       }
     }
     o.take<1>(&x0, x0, c);
-    const uint64_t mine = tid < z.chunks || extra >= 0 ? rank_key(o.m, ~0u) : 0;
-    o = over_workgroup(o, part, c);
+    if (a.top) offer_lane(top, turn, tid < z.chunks || extra >= 0 ? (uint32_t)(rank_key(o.m, 0) >> 32) : 0);
+    o = over_workgroup(o, part[turn], c);
     const bool bad = o.sum != o.sum;
     const auto find = [&]() {
-      return find_top(top, mine, a.top, [&](uint64_t bound) {
-        const auto offer = [&](float x, int v) {
-          const uint64_t key = rank_key(x, (uint32_t)v);
-          if (key >= bound) add_found(top, key);
-        };
-        if (extra >= 0) offer(x0, extra);
-        for (int mark = 0; mark * per_mark < groups; ++mark) {
-          if (rank_key(top.mark[mark][tid], 0) < bound) continue;
-          const int g1 = (mark + 1) * per_mark < groups ? (mark + 1) * per_mark : groups;
-          for (int ch = mark * per_mark * kThreads * kUnroll + tid; ch < g1 * kThreads * kUnroll && ch < z.chunks; ch += kThreads) {
-            float x[N];
-            unpack(z.body[ch], x, (const T*)nullptr);
+      return find_top(top, turn, a.top, [&](uint64_t bound, auto add) {
+        const float least = least_logit(bound);
+        if (extra >= 0 && rank_key(x0, (uint32_t)extra) >= bound) add(rank_key(x0, (uint32_t)extra));
+        for (int g = 0; g < groups; ++g) {
+          if (top.mark[g / per_mark][tid] < least) continue;
+          const int at = g * kThreads * kUnroll + tid;
+          if (groups > 1) load(at);         // (else still at hand)
+          uint32_t reach = 0;               // a bit for each element
 #pragma unroll
-            for (int e = 0; e < N; ++e) offer(x[e], z.from + ch * N + e);
+          for (int u = 0; u < kUnroll; ++u) {
+            float x[N];
+            unpack(raw[u], x, (const T*)nullptr);
+#pragma unroll
+            for (int e = 0; e < N; ++e) reach |= (x[e] >= least && at + u * kThreads < z.chunks ? 1u : 0u) << (u * N + e);
+          }
+          for (; reach; reach &= reach - 1) {
+            const int e = __builtin_ctz(reach), v = z.from + (at + e / N * kThreads) * N + e % N;
+            const uint64_t key = rank_key(as_float(z.z[v]), (uint32_t)v);
+            if (key >= bound) add(key);
           }
         }
       });
@@ -294,54 +370,40 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
       const int n = bad ? 0 : find();
       uint64_t* const keys = a.keys + i * a.top;
       for (int k = tid; k < n; k += kThreads) {
-        const int r = rank_among(top.found, n, top.found[k], k);
+        const int r = rank_among(top.found, n, top.found[k]);
         if (r < a.top) keys[r] = top.found[k];
       }
       for (int k = n + tid; k < a.top; k += kThreads) keys[k] = 0;
     } else {
-      const RowAnswer<T> answer(a, row, o);
-      if (!a.top || bad) continue;
-      const int n = find();
-      for (int k = tid; k < n; k += kThreads) {
-        const uint32_t id = ~(uint32_t)top.found[k];
-        const int r = rank_among(top.found, n, top.found[k], k);
-        if (r < a.top) put_top(a, row, r, id, answer.of(id));
+      answer.put(o);
+      if (a.top && !bad) {
+        const int n = find();
+        answer.put_top(top.found, n);
       }
     }
   }
-}
-
-// parts[0, n), joined by each wavefront by itself
-template <class S>
-__device__ __forceinline__ S join_parts(const S* parts, int n, S o, float c) {
-  for (int k = (int)threadIdx.x & 63; k < n; k += 64) o.join(parts[k], c);
-  o = over_wavefront(o, c);
-  S one = o;                     // (the first lane's: the lanes' own may differ by a rounding)
-  uint32_t* const w = (uint32_t*)&one;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(S) / 4); ++i) w[i] = __builtin_amdgcn_readfirstlane(((const uint32_t*)&o)[i]);
-  return one;
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) {
   __shared__ TopLds top;
   const int tid = (int)threadIdx.x, n_keys = a.segs * a.top;
-  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  int turn = 0;
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    RowAnswer<T> answer(a, row);
     const uint64_t* const keys = a.keys + row * n_keys;
     uint64_t mine = 0;
     for (int k = tid; k < n_keys; k += kThreads) mine = keys[k] > mine ? keys[k] : mine;
-    const RowAnswer<T> answer(a, row, join_parts(a.parts + row * a.segs, a.segs, Online{-INFINITY, 0.0f, 0.0f}, a.scale * kLog2E));
-    if (!a.top || answer.bad) continue;
-    const int n = find_top(top, mine, a.top, [&](uint64_t bound) {
+    if (a.top) offer_lane(top, turn, (uint32_t)(mine >> 32));
+    answer.put(join_parts(a.parts + row * a.segs, a.segs, Online{-INFINITY, 0.0f, 0.0f}, a.scale * kLog2E));
+    if (!a.top) continue;
+    __syncthreads();
+    if (answer.bad) continue;
+    const int n = find_top(top, turn, a.top, [&](uint64_t bound, auto add) {
       for (int k = tid; k < n_keys; k += kThreads)
-        if (keys[k] && keys[k] >= bound) add_found(top, keys[k]);
+        if (keys[k] && keys[k] >= bound) add(keys[k]);
     });
-    for (int k = tid; k < n; k += kThreads) {
-      const uint32_t id = ~(uint32_t)top.found[k];
-      const int r = rank_among(top.found, n, top.found[k], k);
-      if (r < a.top) put_top(a, row, r, id, answer.of(id));
-    }
+    answer.put_top(top.found, n);
   }
 }
 
@@ -386,8 +448,7 @@ __device__ __forceinline__ void take_teacher(TeacherLds& l, const DistillArgs& a
     beyond |= id[k] >= a.classes;
   }
   if (lane == 0) l.z_label = label >= 0 && label < a.classes ? as_float(z[label]) : 0.0f;
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) most = fmaxf(most, __shfl_xor(most, s, 64));
+  most = max_over_lanes(most);
   if (most == -INFINITY) most = 0.0f;
   float e[kEach];
 #pragma unroll
@@ -396,8 +457,7 @@ __device__ __forceinline__ void take_teacher(TeacherLds& l, const DistillArgs& a
     e[k] = pow2(t[k] * kLog2E);
     mass += e[k];
   }
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) mass += __shfl_xor(mass, s, 64);
+  mass = sum_over_lanes(mass);
   const float log_mass = logf(mass);
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
@@ -432,18 +492,15 @@ struct Sums {
       if (TWO) sum1 += pow2((x[i] - from) * kLog2E);
     }
   }
-  __device__ void join(Sums b, float c) {
-    const float to = fmaxf(m, b.m);
-    raise(to, c);
-    b.raise(to, c);
+  __device__ void add(const Sums& b) {
     sum += b.sum;
     if (TWO) sum1 += b.sum1;
   }
+  __device__ void over_lanes() {
+    sum = sum_over_lanes(sum);
+    if (TWO) sum1 = sum_over_lanes(sum1);
+  }
 };
-template <bool TWO>
-__device__ __forceinline__ Sums<TWO> from_lane(const Sums<TWO>& o, int mask) {
-  return Sums<TWO>{__shfl_xor(o.m, mask, 64), __shfl_xor(o.sum, mask, 64), TWO ? __shfl_xor(o.sum1, mask, 64) : 0.0f};
-}
 
 __device__ __forceinline__ uint4 pack(const float* g, const float*) {
   return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
@@ -481,11 +538,12 @@ __device__ __forceinline__ Sums<TWO> sums_of(const RowSpan<T>& z, int extra, flo
 // the sums of parts of rows, where rows are shared out
 template <class T, bool TWO>
 __global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs a) {
-  __shared__ Sums<TWO> part[kWaves];
-  for (long long i = blockIdx.x; i < a.rows * a.segs; i += gridDim.x) {
+  __shared__ Sums<TWO> part[2][kWaves];
+  int turn = 0;
+  for (long long i = blockIdx.x; i < a.rows * a.segs; i += gridDim.x, turn ^= 1) {
     const long long row = i / a.segs;
     const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes, (int)(i - row * a.segs), a.segs);
-    const Sums<TWO> o = sums_of<T, TWO>(z, z.beside((int)threadIdx.x), first_factor(a), part);
+    const Sums<TWO> o = sums_of<T, TWO>(z, z.beside((int)threadIdx.x), first_factor(a), part[turn]);
     if (threadIdx.x == 0) ((Sums<TWO>*)a.parts)[i] = o;
   }
 }
@@ -534,8 +592,7 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
       float l = 0.0f;
       for (int k = tid; k < a.top && taught; k += 64)
         if (teacher.q[k] != 0.0f) l += teacher.q[k] * (teacher.log_q[k] - ((teacher.z[k] - o.m) * a.scale - log_sum));
-#pragma unroll
-      for (int s = 32; s >= 1; s >>= 1) l += __shfl_xor(l, s, 64);
+      l = sum_over_lanes(l);
       l = taught ? l * wt : 0.0f;
       if (labelled) l += wl * ((TWO ? logf(sum1) : log_sum) - (teacher.z_label - o.m));
       if (tid == 0) a.loss[row] = none ? 0.0f : l;
@@ -630,11 +687,11 @@ int check_grad(const char* who, const void* grad, int32_t dtype, int64_t rows, i
   return CG_OK;
 }
 
-// Parts of a row: where there are few rows, as many as give a launch kEnough workgroups, each with kUnroll chunks for a lane at least.
-constexpr int kEnough = 512;
+// Parts of a row: where there are few rows, as many as give a launch kEnough workgroups, of kUnroll chunks for a lane at least.
+constexpr int kEnough = 512, kPartBytes = kThreads * kUnroll * 16;
 int parts_of(int64_t rows, int64_t classes, int bytes) {
   if (rows <= 0 || rows >= kEnough) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>((kEnough + rows - 1) / rows, classes * bytes / (kThreads * kUnroll * 16)));
+  return (int)std::max<int64_t>(1, std::min<int64_t>((kEnough + rows - 1) / rows, (classes * bytes + kPartBytes - 1) / kPartBytes));
 }
 
 template <class T>
