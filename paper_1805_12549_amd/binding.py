@@ -491,8 +491,15 @@ def logprobs(logits, labels=None, top: int = 0, temperature: float = 1.0, entrop
     logits: [rows, classes], float32 or bfloat16, any distance between rows.  labels: int64 [rows] or [rows, given], the classes whose log
     probability is wanted (logprob has their shape; negative: absent, 0).  top: so many alternatives per row in falling order, equal ones by
     index (int64 and float32 [rows, top]).  entropy: float32 [rows].  See cg_logprobs in cg_conv.h for rows of -inf, NaN and +inf."""
+    if _calls is not None:
+        out = _calls.logprobs(logits, labels, top, temperature, entropy)
+        if out.__class__ is tuple:
+            return out
+        if out is not None:
+            raise CGError(out, cg_last_error())
+    # (arguments that are not plain tensors, and what is refused)
     dtype, rows, classes, stride = _logits_of("logprobs", logits)
-    dev = logits.device
+    dev, top, temperature = logits.device, int(top), float(temperature)
     given, logprob, given_entropy, top_ids, top_logprobs = 0, None, None, None, None
     if labels is not None:
         if labels.dim() not in (1, 2) or labels.shape[0] != rows:
@@ -538,7 +545,7 @@ def _grad_of(name, logits, grad, rows, classes, stride):
     """The tensor that takes the gradient: a given one, or a new one whose rows are aligned to 16 bytes as the logits' are."""
     if grad is None or grad is True:
         return _strided((rows, classes), (classes + (stride - classes) % (16 // logits.element_size()), 1), dtype=logits.dtype, device=logits.device)
-    if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device or (grad.stride(1) != 1 and classes > 1):
+    if not isinstance(grad, torch.Tensor) or grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != logits.device or (grad.stride(1) != 1 and classes > 1):
         _refuse(name, "grad must be of the logits' type and shape beside them, the classes of a row side by side")
     return grad
 
@@ -554,8 +561,15 @@ def distill(logits, top_ids, top_logits, labels=None, *, teacher_weight: float =
     stats: what distill_backward takes for the same gradient later on.  The usual factor temperature^2 is the caller's to put into
     teacher_weight.  See cg_distill_forward in cg_conv.h for rows of -inf, NaN and +inf and for labels and ids outside the classes."""
     name = "distill"
+    if _calls is not None:
+        out = _calls.distill(logits, None, top_ids, top_logits, labels, teacher_weight, label_weight, temperature, grad, grad_loss)
+        if out.__class__ is tuple:
+            return out
+        if out is not None:
+            raise CGError(out, cg_last_error())
     dtype, rows, classes, stride = _logits_of(name, logits)
     ids_ptr, top_ptr, top, labels_ptr = _teacher_of(name, logits, rows, top_ids, top_logits, labels)
+    teacher_weight, label_weight, temperature = float(teacher_weight), float(label_weight), float(temperature)
     up_ptr = _beside(name, "grad_loss", grad_loss, torch.float32, (rows,), logits.device)
     want = grad is not None and grad is not False
     grad = _grad_of(name, logits, grad, rows, classes, stride) if want else None
@@ -579,8 +593,15 @@ def distill_backward(logits, stats, top_ids, top_logits, labels=None, *, teacher
                      temperature: float = 1.0, grad=None, grad_loss=None):
     """The gradient of distill's losses with respect to the logits, times grad_loss, from the stats of the forward call and its arguments."""
     name = "distill_backward"
+    if _calls is not None and stats is not None:
+        out = _calls.distill(logits, stats, top_ids, top_logits, labels, teacher_weight, label_weight, temperature, grad, grad_loss)
+        if out.__class__ is int:
+            raise CGError(out, cg_last_error())
+        if out is not None:
+            return out
     dtype, rows, classes, stride = _logits_of(name, logits)
     ids_ptr, top_ptr, top, labels_ptr = _teacher_of(name, logits, rows, top_ids, top_logits, labels)
+    teacher_weight, label_weight, temperature = float(teacher_weight), float(label_weight), float(temperature)
     stats_ptr = _beside(name, "stats", stats, torch.float32, (rows, 3), logits.device)
     up_ptr = _beside(name, "grad_loss", grad_loss, torch.float32, (rows,), logits.device)
     grad = _grad_of(name, logits, grad, rows, classes, stride)

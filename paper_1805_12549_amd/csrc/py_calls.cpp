@@ -144,6 +144,182 @@ PyObject* empty_bf16(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// What the operators behind the classifier are given, as binding.py checks it; false: something that it has to look at (and to refuse, as a rule)
+struct Logits {
+  const at::Tensor* t = nullptr;
+  int32_t dtype = 0;
+  int64_t rows = 0, classes = 0, stride = 0;
+  bool take(PyObject* o) {
+    if (!plain_tensor(o)) return false;
+    t = &THPVariable_Unpack(o);
+    if (t->unsafeGetTensorImpl()->has_symbolic_sizes_strides() || t->dim() != 2 || !t->is_cuda() || t->get_device() != c10::hip::current_device()) return false;
+    if (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16) return false;
+    dtype = t->scalar_type() == at::kFloat ? CG_F32 : CG_BF16;
+    rows = t->size(0), classes = t->size(1), stride = t->stride(0);
+    return classes > 0 && classes <= INT32_MAX && (classes == 1 || t->stride(1) == 1);
+  }
+  at::TensorOptions like(at::ScalarType type) const { return at::TensorOptions().device(t->device()).dtype(type); }
+  // a contiguous tensor of that type beside the logits, or None
+  bool beside(PyObject* o, at::ScalarType type, at::IntArrayRef sizes, const void*& ptr) const {
+    if (o == Py_None) return true;
+    if (!plain_tensor(o)) return false;
+    const at::Tensor& b = THPVariable_Unpack(o);
+    if (b.unsafeGetTensorImpl()->has_symbolic_sizes_strides() || b.scalar_type() != type || b.device() != t->device() || b.sizes() != sizes ||
+        !b.is_contiguous())
+      return false;
+    ptr = b.data_ptr();
+    return true;
+  }
+  // where the gradient goes: None or True (a new tensor whose rows are aligned to 16 bytes as the logits' are) or a tensor
+  bool gradient(PyObject* o, at::Tensor& grad) const {
+    if (o == Py_None || o == Py_True) {
+      const int64_t step = classes + (((stride - classes) % (dtype == CG_F32 ? 4 : 8)) + 8) % (dtype == CG_F32 ? 4 : 8);
+      grad = at::empty_strided({rows, classes}, {step, 1}, like(t->scalar_type()));
+      return true;
+    }
+    if (!plain_tensor(o)) return false;
+    grad = THPVariable_Unpack(o);
+    return !grad.unsafeGetTensorImpl()->has_symbolic_sizes_strides() && grad.scalar_type() == t->scalar_type() && grad.sizes() == t->sizes() &&
+           grad.device() == t->device() && (classes == 1 || grad.stride(1) == 1);
+  }
+};
+
+// a Python float or int, as binding.py passes it to ctypes
+bool number(PyObject* o, float& v) {
+  if (!PyFloat_CheckExact(o) && !PyLong_CheckExact(o)) return false;
+  const double d = PyFloat_AsDouble(o);
+  if (d == -1.0 && PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  v = (float)d;
+  return true;
+}
+
+// logprobs(logits, labels, top, temperature, entropy): (logprob, entropy, top_ids, top_logprobs); an error code; None: not a plain call
+PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (n_args != 5) {
+    PyErr_SetString(PyExc_TypeError, "logprobs takes five arguments");
+    return nullptr;
+  }
+  Logits z;
+  float temperature;
+  if (at::impl::torch_function_mode_enabled() || !z.take(args[0]) || !PyLong_CheckExact(args[2]) || !number(args[3], temperature)) Py_RETURN_NONE;
+  const long long top = PyLong_AsLongLong(args[2]);
+  if (top < 0 || top > z.classes || top > CG_TOP_MAX) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  const int entropy_wanted = PyObject_IsTrue(args[4]);
+  if (entropy_wanted < 0) return nullptr;
+  const void* labels_ptr = nullptr;
+  const at::Tensor* labels = nullptr;
+  int64_t given = 0;
+  if (args[1] != Py_None) {
+    if (!plain_tensor(args[1])) Py_RETURN_NONE;
+    labels = &THPVariable_Unpack(args[1]);
+    if (labels->dim() < 1 || labels->dim() > 2 || labels->size(0) != z.rows || !z.beside(args[1], at::kLong, labels->sizes(), labels_ptr)) Py_RETURN_NONE;
+    given = labels->dim() == 1 ? 1 : labels->size(1);
+    if (given > INT32_MAX) Py_RETURN_NONE;
+  }
+  at::Tensor logprob, entropy, top_ids, top_logprobs;
+  int rc;
+  {
+    const WithoutGil released;
+    const hipStream_t stream = c10::hip::getCurrentHIPStream().stream();
+    if (labels) logprob = at::empty(labels->sizes(), z.like(at::kFloat));
+    if (entropy_wanted) entropy = at::empty({z.rows}, z.like(at::kFloat));
+    if (top) {
+      top_ids = at::empty({z.rows, top}, z.like(at::kLong));
+      top_logprobs = at::empty({z.rows, top}, z.like(at::kFloat));
+    }
+    const size_t need = cg_logprobs_workspace_bytes(z.rows, (int32_t)z.classes, (int32_t)top);
+    const Scratch scratch(need, stream);
+    const auto at = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    rc = cg_logprobs(z.t->data_ptr(), z.dtype, z.rows, (int32_t)z.classes, z.stride, temperature, (const int64_t*)labels_ptr, (int32_t)given, (int32_t)top,
+                     (float*)at(logprob), (float*)at(entropy), (int64_t*)at(top_ids), (float*)at(top_logprobs), scratch.ptr, need, stream);
+  }
+  if (rc != CG_OK) return PyLong_FromLong(rc);
+  PyObject* const out = PyTuple_New(4);
+  if (!out) return nullptr;
+  const at::Tensor* const made[4] = {&logprob, &entropy, &top_ids, &top_logprobs};
+  for (int i = 0; i < 4; ++i) {
+    PyObject* o = Py_None;
+    if (made[i]->defined())
+      o = THPVariable_Wrap(*made[i]);
+    else
+      Py_INCREF(o);
+    PyTuple_SET_ITEM(out, i, o);
+  }
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
+// distill(logits, stats, top_ids, top_logits, labels, teacher_weight, label_weight, temperature, grad, grad_loss): (loss, stats, grad), or with stats
+// given the gradient alone; an error code; None: not a plain call
+PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (n_args != 10) {
+    PyErr_SetString(PyExc_TypeError, "distill takes ten arguments");
+    return nullptr;
+  }
+  Logits z;
+  float w_teacher, w_label, temperature;
+  if (at::impl::torch_function_mode_enabled() || !z.take(args[0]) || !number(args[5], w_teacher) || !number(args[6], w_label) ||
+      !number(args[7], temperature))
+    Py_RETURN_NONE;
+  int64_t top = 0;
+  if ((args[2] == Py_None) != (args[3] == Py_None)) Py_RETURN_NONE;
+  if (args[2] != Py_None) {
+    if (!plain_tensor(args[2]) || THPVariable_Unpack(args[2]).dim() != 2) Py_RETURN_NONE;
+    top = THPVariable_Unpack(args[2]).size(1);
+    if (top > CG_TOP_MAX) Py_RETURN_NONE;
+  }
+  const void *ids = nullptr, *top_logits = nullptr, *labels = nullptr, *up = nullptr, *given_stats = nullptr;
+  if (!z.beside(args[2], at::kLong, {z.rows, top}, ids) || !z.beside(args[3], at::kFloat, {z.rows, top}, top_logits) ||
+      !z.beside(args[4], at::kLong, {z.rows}, labels) || !z.beside(args[9], at::kFloat, {z.rows}, up) || !z.beside(args[1], at::kFloat, {z.rows, 3}, given_stats))
+    Py_RETURN_NONE;
+  const bool backward = args[1] != Py_None, want = backward || (args[8] != Py_None && args[8] != Py_False);
+  at::Tensor grad, loss, stats;
+  if (want && !z.gradient(args[8], grad)) Py_RETURN_NONE;
+  int rc;
+  {
+    const WithoutGil released;
+    const hipStream_t stream = c10::hip::getCurrentHIPStream().stream();
+    if (backward) {
+      rc = cg_distill_backward(z.t->data_ptr(), z.dtype, z.rows, (int32_t)z.classes, z.stride, temperature, (const int64_t*)ids, (const float*)top_logits,
+                               (int32_t)top, (const int64_t*)labels, w_teacher, w_label, (const float*)given_stats, (const float*)up, grad.data_ptr(),
+                               grad.stride(0), stream);
+    } else {
+      loss = at::empty({z.rows}, z.like(at::kFloat));
+      stats = at::empty({z.rows, 3}, z.like(at::kFloat));
+      const size_t need = cg_distill_workspace_bytes(z.rows, (int32_t)z.classes);
+      const Scratch scratch(need, stream);
+      rc = cg_distill_forward(z.t->data_ptr(), z.dtype, z.rows, (int32_t)z.classes, z.stride, temperature, (const int64_t*)ids, (const float*)top_logits,
+                              (int32_t)top, (const int64_t*)labels, w_teacher, w_label, (float*)loss.data_ptr(), (float*)stats.data_ptr(),
+                              (const float*)up, want ? grad.data_ptr() : nullptr, want ? grad.stride(0) : 0, scratch.ptr, need, stream);
+    }
+  }
+  if (rc != CG_OK) return PyLong_FromLong(rc);
+  PyObject* g = want && plain_tensor(args[8]) ? args[8] : Py_None;
+  if (want && g == Py_None)
+    g = THPVariable_Wrap(grad);
+  else
+    Py_INCREF(g);
+  if (backward) return g;
+  PyObject* const out = PyTuple_New(3);
+  if (!out) {
+    Py_DECREF(g);
+    return nullptr;
+  }
+  PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(loss));
+  PyTuple_SET_ITEM(out, 1, THPVariable_Wrap(stats));
+  PyTuple_SET_ITEM(out, 2, g);
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
 int layer_init(PyObject* self, PyObject* args, PyObject*) {
   Layer* const l = (Layer*)self;
   unsigned long long handle;
@@ -164,6 +340,9 @@ PyTypeObject layer_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyMethodDef methods[] = {
     {"forward", (PyCFunction)(void (*)(void))forward, METH_FASTCALL, "forward(layer, stream, x, residual, y, bitmap, counts)"},
     {"empty_bf16", (PyCFunction)(void (*)(void))empty_bf16, METH_FASTCALL, "empty_bf16(like, *sizes)"},
+    {"logprobs", (PyCFunction)(void (*)(void))logprobs, METH_FASTCALL, "logprobs(logits, labels, top, temperature, entropy)"},
+    {"distill", (PyCFunction)(void (*)(void))distill, METH_FASTCALL,
+     "distill(logits, stats, top_ids, top_logits, labels, teacher_weight, label_weight, temperature, grad, grad_loss)"},
     {nullptr, nullptr, 0, nullptr},
 };
 

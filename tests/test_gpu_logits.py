@@ -389,6 +389,37 @@ def test_rows_beyond_two_to_the_31_elements():
         assert torch.allclose(g[picked].float(), w.float(), rtol=2.0 ** -7 if g.dtype == torch.bfloat16 else 1e-5, atol=1e-12)
 
 
+def test_with_and_without_the_calls_extension(monkeypatch):
+    """Both ways of marshalling: the same outputs, and their layouts too."""
+    if B._calls is None:
+        pytest.skip("the extension is not built")
+    rng = np.random.default_rng(8)
+    z = rows_of(rng, 5, 1003, "bf16", pad=3)
+    ids, t, labels = [torch.from_numpy(a).cuda() for a in teacher_of(rng, 5, 1003, 20, absent=True)]
+    up = torch.rand(5, device="cuda")
+
+    def every():
+        kw = dict(teacher_weight=2, label_weight=0.5, temperature=2.0)
+        loss, stats, grad = B.distill(z, ids, t, labels, grad=True, grad_loss=up, **kw)
+        into = torch.zeros_like(grad)
+        assert B.distill(z, ids, t, labels, grad=into, **kw)[2] is into and B.distill_backward(z, stats, ids, t, labels, grad=into, grad_loss=up, **kw) is into
+        return [*B.logprobs(z, labels, top=7, temperature=2), *B.logprobs(z, ids, entropy=False)[:1], loss, stats, grad, into,
+                B.distill(z, None, None, labels, teacher_weight=0.0, label_weight=1.0)[0], B.distill_backward(z, stats, ids, t, labels, **kw)]
+
+    want = every()
+    assert B.distill(z, ids, t)[2] is None and B.distill(z, ids, t, grad=False)[2] is None
+    calls = B._calls
+    monkeypatch.setattr(B, "_calls", None)
+    for w, g in zip(want, every()):
+        assert w.shape == g.shape and w.stride() == g.stride() and w.dtype == g.dtype and same_bits(w, g)
+    # what the extension leaves to Python
+    assert calls.logprobs(z, labels, 2000, 1.0, True) is None and calls.logprobs(z.half(), None, 0, 1.0, True) is None
+    assert calls.logprobs(z, labels.int(), 0, 1.0, True) is None and calls.logprobs(z.t(), None, 0, 1.0, True) is None
+    assert isinstance(calls.logprobs(z, None, 0, -1.0, True), int)
+    assert calls.distill(z, None, ids, t[:4], labels, 1.0, 0.0, 1.0, None, None) is None
+    assert calls.distill(z, None, ids, t, None, 1.0, 0.0, "1", None, None) is None
+
+
 def test_refusals_on_the_gpu():
     z = torch.zeros((4, 100), device="cuda")
     i64 = lambda *s: torch.zeros(s, dtype=torch.int64, device="cuda")  # noqa: E731
