@@ -151,14 +151,14 @@ __device__ __forceinline__ S over_wavefront(S o, float c) {
   return o;
 }
 // Every thread gets the result.  `part`: one value for each wavefront, not those of the row before.
-template <class S>
+template <int kOf = kWaves, class S>
 __device__ __forceinline__ S over_workgroup(S o, S* part, float c) {
   o = over_wavefront(o, c);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = o;
   __syncthreads();
   o = part[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) join(o, part[w], c);
+  for (int w = 1; w < kOf; ++w) join(o, part[w], c);
   return o;
 }
 // parts[0, n), joined by each wavefront by itself
@@ -426,8 +426,9 @@ struct DistillArgs {
 
 // The teacher's side of a row and the logits that its terms ask for, taken by the first wavefront while the others start on the row.
 struct TeacherLds {
-  int64_t id[CG_TOP_MAX];        // -1: absent
-  float q[CG_TOP_MAX], log_q[CG_TOP_MAX], z[CG_TOP_MAX];
+  alignas(16) int id[CG_TOP_MAX];        // -1: absent, or no class
+  alignas(16) float q[CG_TOP_MAX];
+  float log_q[CG_TOP_MAX], z[CG_TOP_MAX];
   float mass, z_label;
   int beyond;                    // an id names no class
 };
@@ -462,11 +463,11 @@ __device__ __forceinline__ void take_teacher(TeacherLds& l, const DistillArgs& a
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     const int at = lane + 64 * k;
-    if (at >= a.top) continue;
-    l.id[at] = id[k];
+    const bool named = id[k] >= 0 && id[k] < a.classes;
+    l.id[at] = named ? (int)id[k] : -1;
     l.q[at] = mass != 0.0f ? e[k] / mass : 0.0f;
     l.log_q[at] = t[k] - log_mass;
-    l.z[at] = id[k] >= 0 && id[k] < a.classes ? as_float(z[id[k]]) : 0.0f;
+    l.z[at] = named ? as_float(z[id[k]]) : 0.0f;
   }
   if (lane == 0) l.mass = mass;
   beyond = __any(beyond);
@@ -515,24 +516,112 @@ __device__ __forceinline__ uint4 pack(const float* g, const uint16_t*) {
 // The exponentials' factor of the first sum (the only one, or the teacher's).
 __device__ __forceinline__ float first_factor(const DistillArgs& a) { return a.w_teacher != 0.0f ? a.scale * kLog2E : kLog2E; }
 
+template <class T, int kOf, bool TWO>
+__device__ __forceinline__ void take_chunks(Sums<TWO>& o, const uint4* raw, float c) {
+  constexpr int N = RowSpan<T>::kPer;
+  float x[kOf * N], most = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < kOf; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
+#pragma unroll
+  for (int i = 0; i < kOf * N; ++i) most = fmaxf(most, x[i]);
+  o.template take<kOf * N>(x, most, c);
+}
+
 template <class T, bool TWO>
 __device__ __forceinline__ Sums<TWO> sums_of(const RowSpan<T>& z, int extra, float c, Sums<TWO>* part) {
-  constexpr int N = RowSpan<T>::kPer;
   Sums<TWO> o{-INFINITY, 0.0f, 0.0f};
   const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
   for (int at = (int)threadIdx.x; at < z.chunks; at += kThreads * kUnroll) {
     uint4 raw[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
-    float x[kUnroll * N], most = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
-#pragma unroll
-    for (int i = 0; i < kUnroll * N; ++i) most = fmaxf(most, x[i]);
-    o.template take<kUnroll * N>(x, most, c);
+    take_chunks<T, kUnroll>(o, raw, c);
   }
   o.template take<1>(&x0, x0, c);
   return over_workgroup(o, part, c);
+}
+
+template <bool TWO>
+__device__ __forceinline__ void put_stats(const DistillArgs& a, long long row, const Sums<TWO>& o) {
+  a.stats[row * 3] = o.m;
+  a.stats[row * 3 + 1] = a.w_label == 0.0f ? NAN : TWO ? o.sum1 : o.sum;
+  a.stats[row * 3 + 2] = a.w_teacher == 0.0f ? NAN : o.sum;
+}
+
+// What a row's terms are, once its teacher and its sums are known.
+template <bool TWO>
+struct Terms {
+  bool taught, labelled, none;
+  float wt, wl;            // weights; NaN where a label or an entry is no number or names no class
+  float ct, cl;            // and with the gradient from above and 1 / temperature
+  float kt, k1;            // the exponentials' factors in the gradient
+  float m, c;
+  __device__ Terms(const DistillArgs& a, long long row, const TeacherLds& l, const Sums<TWO>& o, int64_t label, float up) {
+    taught = a.w_teacher != 0.0f && (l.mass != 0.0f || l.beyond);
+    labelled = label >= 0;
+    none = o.sum == 0.0f || (!taught && !labelled);
+    wt = !taught ? 0.0f : l.beyond || l.mass != l.mass ? NAN : a.w_teacher;
+    wl = !labelled ? 0.0f : label >= a.classes ? NAN : a.w_label;
+    ct = up * wt * a.scale, cl = up * wl;
+    k1 = TWO && labelled ? cl / o.sum1 : 0.0f;
+    kt = (taught ? ct / o.sum : 0.0f) + (!TWO && labelled ? cl / o.sum : 0.0f);
+    m = o.m, c = first_factor(a);
+  }
+  // the probabilities' part of a class's gradient
+  __device__ float slope(float x) const {
+    const float y = x - m, p = kt * pow2(y * c);
+    return none ? 0.0f : TWO ? fmaf(k1, pow2(y * kLog2E), p) : p;
+  }
+};
+
+// The loss of a row, by its first wavefront.
+template <bool TWO>
+__device__ __forceinline__ void put_loss(const DistillArgs& a, long long row, const TeacherLds& l, const Sums<TWO>& o, const Terms<TWO>& t) {
+  const float log_sum = logf(o.sum);
+  float loss = 0.0f;
+  for (int k = (int)threadIdx.x; k < a.top && t.taught; k += 64)
+    if (l.q[k] != 0.0f) loss += l.q[k] * (l.log_q[k] - ((l.z[k] - o.m) * a.scale - log_sum));
+  loss = sum_over_lanes(loss);
+  loss = t.taught ? loss * t.wt : 0.0f;
+  if (t.labelled) loss += t.wl * ((TWO ? logf(o.sum1) : log_sum) - (l.z_label - o.m));
+  if (threadIdx.x == 0) a.loss[row] = t.none ? 0.0f : loss;
+}
+
+// The class of the teacher's entry or of the label that this thread writes again at the end, and the gradient there, in full and rounded once.
+template <class T, bool TWO>
+struct Named {
+  int at;                  // -1: none
+  float value;
+  template <class Here>
+  __device__ Named(const DistillArgs& a, const TeacherLds& l, const Terms<TWO>& t, int64_t label, Here here) {
+    const int tid = (int)threadIdx.x;
+    const int64_t id = tid < a.top ? l.id[tid] : tid == a.top ? label : -1;
+    at = id >= 0 && !t.none && here(id) ? (int)id : -1;
+    if (at < 0) return;
+    float minus = 0.0f;
+    if (t.taught) {
+#pragma unroll 1
+      for (int k = 0; k < a.top; k += 4) {       // (entries behind the last one are absent)
+        const int4 ids = *(const int4*)(l.id + k);
+        const float4 q = *(const float4*)(l.q + k);
+        minus += (ids.x == at ? q.x : 0.0f) + (ids.y == at ? q.y : 0.0f) + (ids.z == at ? q.z : 0.0f) + (ids.w == at ? q.w : 0.0f);
+      }
+    }
+    value = t.slope(tid < a.top ? l.z[tid] : l.z_label) - t.ct * minus - (t.labelled && at == label ? t.cl : 0.0f);
+  }
+  __device__ void put_into(T* g) const {
+    if (at >= 0) put(g + at, value);
+  }
+};
+
+template <class T, bool TWO>
+__device__ __forceinline__ uint4 slopes_of(const Terms<TWO>& t, const uint4& raw) {
+  constexpr int N = RowSpan<T>::kPer;
+  float x[N];
+  unpack(raw, x, (const T*)nullptr);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = t.slope(x[i]);
+  return pack(x, (const T*)nullptr);
 }
 
 // the sums of parts of rows, where rows are shared out
@@ -549,9 +638,8 @@ __global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs a) {
 }
 
 // Loss and gradient of a row, or of one of `segs` parts of it.  One pass for the sums (none where the call brings them, or where a launch before
-// has formed those of parts), one that writes the gradient: for every class the
-// probabilities' part; then the classes that the label or the teacher names are written again, in full and rounded once.  TWO: both terms
-// are there at different temperatures, that is two sums and two exponentials an element.
+// has formed those of parts), one that writes the gradient: for every class the probabilities' part; then the classes that the label or the teacher
+// names are written again.  TWO: both terms are there at different temperatures, that is two sums and two exponentials an element.
 template <class T, bool TWO>
 __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
   __shared__ Sums<TWO> part[kWaves];
@@ -564,85 +652,135 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
     const int seg = (int)(i - row * a.segs);
     const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes, seg, a.segs);
     const int64_t label = a.labels && a.w_label != 0.0f ? a.labels[row] : -1;
+    const float up = a.grad && a.grad_loss ? a.grad_loss[row] : 1.0f;
     const int extra = z.beside(tid);
     if (tid < 64) take_teacher(teacher, a, row, z.z, label);
     Sums<TWO> o{-INFINITY, 0.0f, 0.0f};
+    uint4 raw[kUnroll];
+    float x0 = 0.0f;
+    const auto load = [&](int at) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        if (at + u * kThreads < z.chunks) raw[u] = z.body[at + u * kThreads];
+    };
+    const bool known = a.given_stats || a.n_parts;
+    if (!known) o = sums_of<T, TWO>(z, extra, c, part);
+    if (a.grad) {          // on their way while the sums are joined and the teacher is waited for
+      load(tid);
+      if (extra >= 0) x0 = as_float(z.z[extra]);
+    }
     if (a.given_stats) {
       const float* const st = a.given_stats + row * 3;
       o = Sums<TWO>{st[0], a.w_teacher != 0.0f ? st[2] : st[1], st[1]};
-      __syncthreads();
     } else if (a.n_parts) {
       o = join_parts((const Sums<TWO>*)a.parts + row * a.n_parts, a.n_parts, o, c);
-      __syncthreads();
-    } else {
-      o = sums_of<T, TWO>(z, extra, c, part);
     }
-    if (a.stats && seg == 0 && tid == 0) {
-      a.stats[row * 3] = o.m;
-      a.stats[row * 3 + 1] = a.w_label == 0.0f ? NAN : TWO ? o.sum1 : o.sum;
-      a.stats[row * 3 + 2] = a.w_teacher == 0.0f ? NAN : o.sum;
-    }
-    const float sum1 = TWO ? o.sum1 : o.sum;
-    const bool taught = a.w_teacher != 0.0f && (teacher.mass != 0.0f || teacher.beyond), labelled = label >= 0;
-    const float wt = !taught ? 0.0f : teacher.beyond || teacher.mass != teacher.mass ? NAN : a.w_teacher;
-    const float wl = !labelled ? 0.0f : label >= a.classes ? NAN : a.w_label;
-    const bool none = o.sum == 0.0f || (!taught && !labelled);       // nothing to learn from this row
-    if (a.loss && seg == 0 && tid < 64) {
-      const float log_sum = logf(o.sum);
-      float l = 0.0f;
-      for (int k = tid; k < a.top && taught; k += 64)
-        if (teacher.q[k] != 0.0f) l += teacher.q[k] * (teacher.log_q[k] - ((teacher.z[k] - o.m) * a.scale - log_sum));
-      l = sum_over_lanes(l);
-      l = taught ? l * wt : 0.0f;
-      if (labelled) l += wl * ((TWO ? logf(sum1) : log_sum) - (teacher.z_label - o.m));
-      if (tid == 0) a.loss[row] = none ? 0.0f : l;
-    }
+    if (known) __syncthreads();
+    if (a.stats && seg == 0 && tid == 0) put_stats(a, row, o);
+    const Terms<TWO> terms(a, row, teacher, o, label, up);
+    if (a.loss && seg == 0 && tid < 64) put_loss(a, row, teacher, o, terms);
     if (a.grad) {
       T* const g = (T*)a.grad + row * a.grad_stride;
-      const float up = a.grad_loss ? a.grad_loss[row] : 1.0f;
-      const float ct = up * wt * a.scale, cl = up * wl;
-      // factors of the exponentials
-      const float k1 = TWO && labelled ? cl / sum1 : 0.0f, kt = (taught ? ct / o.sum : 0.0f) + (!TWO && labelled ? cl / o.sum : 0.0f);
-      const auto slope = [&](float x) {
-        const float y = x - o.m, p = kt * pow2(y * c);
-        return none ? 0.0f : TWO ? fmaf(k1, pow2(y * kLog2E), p) : p;
-      };
-      // what the thread of an entry or of the label puts there at the end
-      float mine = 0.0f;
-      const int64_t to = tid < a.top ? teacher.id[tid] : tid == a.top ? label : -1;
-      const bool named = to >= 0 && !none && z.holds(to);
-      if (named) {
-        float minus = 0.0f;
-        for (int k = 0; k < a.top && taught; ++k) minus += teacher.id[k] == to ? teacher.q[k] : 0.0f;
-        mine = slope(tid < a.top ? teacher.z[tid] : teacher.z_label) - ct * minus - (labelled && to == label ? cl : 0.0f);
-      }
-      if (extra >= 0) put(g + extra, slope(as_float(z.z[extra])));
+      const Named<T, TWO> named(a, teacher, terms, label, [&](int64_t v) { return z.holds(v); });
       const bool same_phase = (((uintptr_t)g ^ (uintptr_t)z.z) & 15) == 0;
+      if (extra >= 0) put(g + extra, terms.slope(x0));
       for (int at = tid; at < z.chunks; at += kThreads * kUnroll) {
-        uint4 raw[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : make_uint4(0, 0, 0, 0);
+        if (at != tid) load(at);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
           const int ch = at + u * kThreads;
-          if (ch >= z.chunks) break;
-          float x[N];
-          unpack(raw[u], x, (const T*)nullptr);
-#pragma unroll
-          for (int i = 0; i < N; ++i) x[i] = slope(x[i]);
+          if (ch >= z.chunks) continue;
+          const uint4 v = slopes_of<T, TWO>(terms, raw[u]);
           T* const out = g + z.from + ch * N;
           if (same_phase) {
-            *(uint4*)out = pack(x, (const T*)nullptr);
+            *(uint4*)out = v;
           } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) put(out + i, x[i]);
+            for (int e = 0; e < N; ++e) out[e] = ((const T*)&v)[e];
           }
         }
       }
       __syncthreads();
-      if (named) put(g + to, mine);
+      named.put_into(g);
     }
     __syncthreads();       // (the next row's teacher takes the place of this one's)
+  }
+}
+
+// Loss and gradient of rows of up to kHeld * OF chunks in one pass: a row stays in the registers of its workgroup between its sums and its gradient, and as
+// the gradient leaves, the next row's chunks take the registers' place, so that loads and stores are on their way together.  A workgroup walks rows.
+// Rows of logits and gradient have the same alignment to 16 bytes.  Chunks are accessed through buffers of their number: what lies behind the last one
+// is neither read nor written, and no access needs registers for an address.
+constexpr int kHeld = 16;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <class T, bool TWO, int OF>
+__global__ __launch_bounds__(OF, 4) void distill_held_kernel(DistillArgs a) {
+  __shared__ Sums<TWO> part[2][OF / 64];
+  __shared__ TeacherLds teachers[2];
+  constexpr int kTake = sizeof(T) == 2 ? 2 : 4;       // chunks between two looks at the maximum
+  const int tid = (int)threadIdx.x;
+  const float c = first_factor(a);
+  uint4 raw[kHeld];
+  float x0 = 0.0f;
+  int turn = 0;
+  const auto row_at = [&](long long row) { return RowSpan<T>((const T*)a.logits + row * a.stride, a.classes, 0, 1); };
+  const auto chunks_of = [](const void* body, int chunks) { return __builtin_amdgcn_make_buffer_rsrc((void*)body, (short)0, chunks * 16, 0x00027000); };
+  const auto load = [&](__amdgpu_buffer_rsrc_t from, int u) {
+    raw[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, (tid + u * OF) * 16, 0, 0));
+  };
+  const auto load_extra = [&](const RowSpan<T>& z) {
+    const int extra = z.beside(tid);
+    x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
+  };
+  long long row = blockIdx.x;
+  {
+    const RowSpan<T> z = row_at(row);
+    const __amdgpu_buffer_rsrc_t from = chunks_of(z.body, z.chunks);
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u)
+      if (u * OF < z.chunks) load(from, u);
+    load_extra(z);
+  }
+  for (;; turn ^= 1) {
+    TeacherLds& teacher = teachers[turn];
+    const RowSpan<T> z = row_at(row);
+    const int64_t label = a.labels && a.w_label != 0.0f ? a.labels[row] : -1;
+    const float up = a.grad_loss ? a.grad_loss[row] : 1.0f;
+    if (tid < 64) take_teacher(teacher, a, row, z.z, label);
+    Sums<TWO> o{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < kHeld; u += kTake) {
+      if (u * OF >= z.chunks) break;
+      if ((u + kTake) * OF > z.chunks) {
+#pragma unroll
+        for (int v = u; v < u + kTake; ++v)
+          if (tid + v * OF >= z.chunks) raw[v] = all_minus_inf<T>();
+      }
+      take_chunks<T, kTake>(o, raw + u, c);
+    }
+    o.template take<1>(&x0, x0, c);
+    o = over_workgroup<OF / 64>(o, part[turn], c);
+    if (a.stats && tid == 0) put_stats(a, row, o);
+    const Terms<TWO> terms(a, row, teacher, o, label, up);
+    if (tid < 64) put_loss(a, row, teacher, o, terms);
+    T* const g = (T*)a.grad + row * a.grad_stride;
+    const Named<T, TWO> named(a, teacher, terms, label, [&](int64_t v) { return v < a.classes; });
+    if (const int extra = z.beside(tid); extra >= 0) put(g + extra, terms.slope(x0));
+    const long long next = row + gridDim.x;
+    const bool more = next < a.rows;
+    const RowSpan<T> zn = row_at(more ? next : row);
+    const __amdgpu_buffer_rsrc_t to = chunks_of(g + z.from, z.chunks), from = chunks_of(zn.body, more ? zn.chunks : 0);
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      if (u * OF < z.chunks) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, slopes_of<T, TWO>(terms, raw[u])), to, (tid + u * OF) * 16, 0, 0);
+      if (u * OF < zn.chunks) load(from, u);
+    }
+    if (more) load_extra(zn);
+    __syncthreads();
+    named.put_into(g);
+    if (!more) return;
+    row = next;
   }
 }
 
@@ -708,6 +846,18 @@ template <class T, bool TWO>
 void launch_distill_as(DistillArgs a, hipStream_t s) {
   const int segs = parts_of(a.rows, a.classes, sizeof(T));
   a.segs = segs;
+  const int64_t chunks = ((int64_t)a.classes * (int)sizeof(T)) / 16;
+  const bool same_phase = (((uintptr_t)a.grad ^ (uintptr_t)a.logits) & 15) == 0 && (a.rows == 1 || (a.grad_stride - a.stride) * (int)sizeof(T) % 16 == 0);
+  if (segs == 1 && a.grad && !a.given_stats && chunks <= kHeld * 1024 && same_phase) {
+    // workgroups that a compute unit's registers hold at once: 1024 threads on each of 256
+    if (chunks <= kHeld * 256)
+      hipLaunchKernelGGL((distill_held_kernel<T, TWO, 256>), dim3((unsigned)std::min<int64_t>(a.rows, 1024)), dim3(256), 0, s, a);
+    else if (chunks <= kHeld * 512)
+      hipLaunchKernelGGL((distill_held_kernel<T, TWO, 512>), dim3((unsigned)std::min<int64_t>(a.rows, 512)), dim3(512), 0, s, a);
+    else
+      hipLaunchKernelGGL((distill_held_kernel<T, TWO, 1024>), dim3((unsigned)std::min<int64_t>(a.rows, 256)), dim3(1024), 0, s, a);
+    return;
+  }
   if (segs > 1 && !a.given_stats) {
     hipLaunchKernelGGL((distill_part_kernel<T, TWO>), dim3((unsigned)(a.rows * segs)), dim3(kThreads), 0, s, a);
     a.n_parts = segs;
