@@ -246,7 +246,7 @@ int cg_avgpool_fc(const void* x, const void* wfc, const float* bias, float* logi
  * CG_BF16, `row_stride` elements from one row to the next (any, 0 too: every row the same), aligned to their elements only.
  * Class indices are int64.  All pointers are DEVICE pointers, nothing is allocated, work is only enqueued on hip_stream, and
  * arguments are checked before any HIP call.  Sums are held in fp32, whatever the logits' type, and added in an order that
- * depends on the sizes of the call alone: the same call gives the same bits.  A workspace may be NULL where its size is 0, else it is
+ * depends on the sizes and the alignment of the call alone: the same call gives the same bits.  A workspace may be NULL where its size is 0, else it is
  * 256-byte aligned; a captured call keeps its address, so it must stay the graph's own, and calls that may overlap need
  * workspaces of their own.  Outputs must not overlap inputs or each other, but for `grad`, which may be the logits
  * themselves, with their strides.

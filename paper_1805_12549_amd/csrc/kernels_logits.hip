@@ -22,7 +22,7 @@ using cg::bf16_to_float;
 using cg::float_to_bf16;
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
+constexpr int kUnroll = 4;           // chunks that a lane takes at once
 constexpr float kLog2E = 1.44269504088896340736f;
 
 __device__ __forceinline__ float as_float(float v) { return v; }
@@ -105,6 +105,13 @@ __device__ __forceinline__ float sum_over_lanes(float x) {
   return over_lanes(x, [](float a, float b) { return a + b; });
 }
 
+// the chunks at, at + OF, ... of a part; -inf where it has none
+template <int OF, class T>
+__device__ __forceinline__ void load_chunks(const RowSpan<T>& z, int at, uint4 (&raw)[kUnroll]) {
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * OF < z.chunks ? z.body[at + u * OF] : all_minus_inf<T>();
+}
+
 // A softmax in one pass: with m the greatest logit so far, the sum of e = 2^((z - m) c) and the sum of e (z - m) c, c = log2(e) / temperature.
 // A new maximum scales both.  NaN and +inf make the sum NaN; without any class m is -inf and the sum 0.
 struct Online {
@@ -151,11 +158,17 @@ __device__ __forceinline__ S over_wavefront(S o, float c) {
   return o;
 }
 // Every thread gets the result.  `part`: one value for each wavefront, not those of the row before.
-template <int kOf = kWaves, class S>
+template <int kOf = kThreads / 64, class S>
 __device__ __forceinline__ S over_workgroup(S o, S* part, float c) {
   o = over_wavefront(o, c);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = o;
   __syncthreads();
+  if (kOf > 4) {
+    const int lane = (int)threadIdx.x & 63;
+    o = part[lane < kOf ? lane : 0];
+    if (lane >= kOf) o = S{-INFINITY, 0.0f, 0.0f};
+    return over_wavefront(o, c);
+  }
   o = part[0];
 #pragma unroll
   for (int w = 1; w < kOf; ++w) join(o, part[w], c);
@@ -168,16 +181,16 @@ __device__ __forceinline__ S join_parts(const S* parts, int n, S o, float c) {
   return over_wavefront(o, c);
 }
 
-constexpr int kUnroll = 4;           // chunks that a lane has on their way
-constexpr int kMarks = 16;           // stretches of a lane whose greatest logits are kept
-constexpr int kCandidates = 1024;    // at most so many are compared with each other
-
+// What a workgroup of OF threads needs to find the alternatives.
+template <int OF>
 struct TopLds {
-  float mark[kMarks][kThreads];      // of each lane's stretches
-  uint32_t lane[2][kThreads];        // upper halves of the lanes' greatest keys (0: none), for rows in turn
-  int count[2];
+  static constexpr int kMarks = OF == 64 ? 4 : 4096 / OF;         // stretches of a lane whose greatest logits are kept
+  static constexpr int kCandidates = OF == 64 ? 256 : 1024;       // at most so many are compared with each other
+  float mark[kMarks][OF];
+  uint16_t stretch[kMarks * OF];     // those that are looked through
+  uint32_t lane[2][OF];              // upper halves of the lanes' greatest keys (0: none), for rows in turn
+  int count[2], stretches[2];
   alignas(16) uint64_t found[kCandidates];
-  uint64_t bound;
 };
 
 // how many of keys[0, n), all different, are greater than `key`
@@ -191,44 +204,65 @@ __device__ __forceinline__ int rank_among(const uint64_t* keys, int n, uint64_t 
   return j < n ? r + (keys[j] > key) : r;
 }
 
-// What a lane leaves for find_top, before a barrier.
-__device__ __forceinline__ void offer_lane(TopLds& l, int turn, uint32_t upper) {
-  l.lane[turn][threadIdx.x] = upper;
-  if (threadIdx.x == 0) l.count[turn] = 0;
-}
-
-// The `top` greatest keys of a workgroup's lanes, which are all different: found[0, n) holds them, and few others.  scan(bound, add) calls add(key) for
-// every key of this lane from `bound` up.  The top-th of the lanes' greatest, cut to 16 bits, is a bound that at least `top` keys reach; as a
-// rule few more do.  Where `found` does not hold them (equal logits, or a lane that has many of the greatest), the top-th of those
-// that it took, whichever these are, is a higher bound that `top` keys reach, and at least kCandidates - top keys lie below it.
-template <class Scan>
-__device__ int find_top(TopLds& l, int turn, int top, Scan scan) {
-  const int tid = (int)threadIdx.x;
-  uint32_t k[kWaves], cut = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) k[w] = l.lane[turn][w * 64 + (tid & 63)] >> 16;
-#pragma unroll
-  for (int bit = 15; bit >= 0; --bit) {       // every wavefront by itself: bit by bit, as long as `top` lanes reach the number
-    const uint32_t next = cut | 1u << bit;
+// The greatest number that at least `top` of a wavefront's lanes * W keys reach, its highest kBits of kOf bits: bit by bit.
+template <int kBits, int kOf, class K, int W>
+__device__ __forceinline__ K reached_by(const K (&k)[W], int top) {
+  K cut = 0;
+#pragma unroll(kBits == 16 ? 16 : 1)
+  for (int bit = kOf - 1; bit >= kOf - kBits; --bit) {
+    const K next = cut | (K)1 << bit;
     int n = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(k[w] >= next));
-    cut = n >= top ? next : cut;
+    for (int w = 0; w < W; ++w) n += __popcll(__ballot(k[w] >= next));
+    if (n >= top) cut = next;
   }
-  uint64_t bound = (uint64_t)cut << 48;
+  return cut;
+}
+
+// What a lane leaves for find_top, before a barrier.
+template <int OF>
+__device__ __forceinline__ void offer_lane(TopLds<OF>& l, int turn, uint32_t upper) {
+  l.lane[turn][threadIdx.x] = upper;
+  if (threadIdx.x == 0) l.count[turn] = l.stretches[turn] = 0;
+}
+
+template <int OF>
+__device__ __forceinline__ void add_found(TopLds<OF>& l, int turn, uint64_t key) {
+  const int at = atomicAdd(&l.count[turn], 1);
+  if (at < TopLds<OF>::kCandidates) l.found[at] = key;
+}
+
+// The `top` greatest keys of a workgroup's lanes, which are all different: found[0, n) holds them, and few others.  scan(bound) calls add_found for
+// every key from `bound` up, or for more than kCandidates of them.  The top-th of the lanes' greatest keys, cut to 16 bits, is a bound that at least
+// `top` keys reach; as a rule few more do.  Where `found` does not hold them (equal logits, or a lane that has many of the greatest), the same is done
+// with those that it took, whichever these are: the bound then rises above OF - top of them at least.
+template <int OF, class Scan>
+__device__ int find_top(TopLds<OF>& l, int turn, int top, Scan scan) {
+  constexpr int kFull = TopLds<OF>::kCandidates;
+  const int tid = (int)threadIdx.x, lane = tid & 63;
+  uint64_t bound;
+  {
+    uint32_t k[OF / 64];
+#pragma unroll
+    for (int w = 0; w < OF / 64; ++w) k[w] = l.lane[turn][w * 64 + lane];
+    bound = (uint64_t)reached_by<16, 32>(k, top) << 32;
+  }
   for (;;) {
-    scan(bound, [&](uint64_t key) {
-      const int at = atomicAdd(&l.count[turn], 1);
-      if (at < kCandidates) l.found[at] = key;
-    });
+    scan(bound);
     __syncthreads();
     const int n = l.count[turn];
-    if (n <= kCandidates) return n;
-    for (int i = tid; i < kCandidates; i += kThreads)
-      if (rank_among(l.found, kCandidates, l.found[i]) == top - 1) l.bound = l.found[i];
+    if (n <= kFull) return n;
+    constexpr int kLanes = kFull / 4 / 64;
+    uint64_t k[kLanes];
+#pragma unroll
+    for (int w = 0; w < kLanes; ++w) {
+      const uint64_t* const f = l.found + (w * 64 + lane) * 4;
+      const uint64_t a = f[0] > f[1] ? f[0] : f[1], b = f[2] > f[3] ? f[2] : f[3];
+      k[w] = a > b ? a : b;
+    }
+    bound = reached_by<64, 64>(k, top);
     __syncthreads();
-    bound = l.bound;
-    if (tid == 0) l.count[turn] = 0;
+    if (tid == 0) l.count[turn] = l.stretches[turn] = 0;
     __syncthreads();
   }
 }
@@ -237,8 +271,16 @@ __device__ __forceinline__ float logit_of(uint64_t key) {
   const uint32_t up = (uint32_t)(key >> 32);
   return __uint_as_float(up & 0x80000000u ? up ^ 0x80000000u : ~up);
 }
-// the least logit whose keys may reach the bound (below -inf's own there is none)
-__device__ __forceinline__ float least_logit(uint64_t bound) { return (bound >> 32) < 0x00800000u ? -INFINITY : logit_of(bound); }
+
+// A bound as logits and indices meet it: greater logits than `least`, and equal ones up to the class `last`.
+struct Bound {
+  uint64_t key;
+  float least;
+  uint32_t last;
+  __device__ explicit Bound(uint64_t k) : key(k), least((k >> 32) < 0x00800000u ? -INFINITY : logit_of(k)), last(~(uint32_t)k) {}
+  // whether a logit of a class not before `first` may reach it
+  __device__ bool met(float x, uint32_t first) const { return x > least || (x == least && first <= last); }
+};
 
 struct LogprobArgs {
   const void* logits;
@@ -249,12 +291,12 @@ struct LogprobArgs {
   float *logprob, *entropy;
   int64_t* top_ids;
   float* top_logprobs;
-  Online* parts;           // [rows][segs] and their greatest keys [rows][segs][top] (0: fewer than that), where rows are shared out
+  Online* parts;           // [rows][segs] and their greatest keys [rows][top][segs] (0: fewer than that), where rows are shared out
   uint64_t* keys;
 };
 
 // A row's log probabilities.  The logits of given classes are on their way while the row is read.
-template <class T>
+template <class T, int OF>
 struct RowAnswer {
   const LogprobArgs& a;
   const T* z;
@@ -273,12 +315,12 @@ struct RowAnswer {
   __device__ void put(const Online& o) {
     m = o.m, log_sum = logf(o.sum), none = o.sum == 0.0f, bad = o.sum != o.sum;
     const int tid = (int)threadIdx.x;
-    for (int g = tid; g < a.given; g += kThreads) {
+    for (int g = tid; g < a.given; g += OF) {
       if (g != tid) take(g);
       a.logprob[row * a.given + g] = id0 < 0 ? 0.0f : id0 >= a.classes ? NAN : of(z0);
     }
     if (a.entropy && tid == 0) a.entropy[row] = none ? 0.0f : log_sum - o.moment / (o.sum * kLog2E);
-    if (bad && tid < a.top) put_top(tid, -1, NAN);
+    for (int k = tid; bad && k < a.top; k += OF) put_top(k, -1, NAN);
   }
   __device__ float of(float x) const { return none ? -INFINITY : bad ? NAN : (x - m) * a.scale - log_sum; }
   __device__ void put_top(int at, int64_t id, float logprob) const {
@@ -286,7 +328,7 @@ struct RowAnswer {
     a.top_logprobs[row * a.top + at] = logprob;
   }
   __device__ void put_top(const uint64_t* found, int n) const {
-    for (int k = (int)threadIdx.x; k < n; k += kThreads) {
+    for (int k = (int)threadIdx.x; k < n; k += OF) {
       const int r = rank_among(found, n, found[k]);
       if (r < a.top) put_top(r, ~(uint32_t)found[k], of(logit_of(found[k])));
     }
@@ -295,39 +337,38 @@ struct RowAnswer {
 
 // One pass over the row (V elements are read once): every lane keeps its own running maximum and sums.  The alternatives come from what the pass
 // leaves behind: the lanes' maxima give a bound that is reached by little more than `top` classes, the maxima of each lane's stretches say where those
-// lie, and only such stretches are read again.  PART: a workgroup takes one of `segs` parts of a row, and leaves its sums and keys to
+// lie, and only such stretches are read again, all at once.  PART: a workgroup takes one of `segs` parts of a row, and leaves its sums and keys to
 // logprobs_join_kernel.
-template <class T, bool PART>
-__global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
-  __shared__ Online part[2][kWaves];
-  __shared__ TopLds top;
-  constexpr int N = RowSpan<T>::kPer;
+template <class T, bool PART, int OF>
+__global__ __launch_bounds__(OF) void logprobs_kernel(LogprobArgs a) {
+  __shared__ Online part[2][OF / 64];
+  __shared__ TopLds<OF> top;
+  constexpr int N = RowSpan<T>::kPer, kMarks = TopLds<OF>::kMarks;
   const int tid = (int)threadIdx.x, segs = PART ? a.segs : 1;
   const float c = a.scale * kLog2E;
   int turn = 0;
   for (long long i = blockIdx.x; i < a.rows * segs; i += gridDim.x, turn ^= 1) {
     const long long row = PART ? i / segs : i;
-    RowAnswer<T> answer(a, row);
-    const RowSpan<T> z(answer.z, a.classes, PART ? (int)(i - row * segs) : 0, segs);
-    const int groups = (z.chunks + kThreads * kUnroll - 1) / (kThreads * kUnroll);
+    const int seg = PART ? (int)(i - row * segs) : 0;
+    RowAnswer<T, OF> answer(a, row);
+    const RowSpan<T> z(answer.z, a.classes, seg, segs);
+    const int groups = (z.chunks + OF * kUnroll - 1) / (OF * kUnroll);
     const int per_mark = (groups + kMarks - 1) / kMarks;       // groups of a stretch
     const int extra = z.beside(tid);
     Online o{-INFINITY, 0.0f, 0.0f};
     const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
     float stretch = -INFINITY;
-    uint4 raw[kUnroll];
-    const auto load = [&](int at) {
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
-    };
+    uint4 raw[kUnroll], first;
+    load_chunks<OF>(z, tid, raw);
+    first = raw[0];
     for (int g = 0, in = 0, mark = 0; g < groups; ++g) {
-      load(g * kThreads * kUnroll + tid);
       float x[kUnroll * N], most = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
+      if (g + 1 < groups) load_chunks<OF>(z, (g + 1) * OF * kUnroll + tid, raw);      // on their way meanwhile
 #pragma unroll
       for (int e = 0; e < kUnroll * N; ++e) most = fmaxf(most, x[e]);
-      o.take<kUnroll * N>(x, most, c);
+      o.template take<kUnroll * N>(x, most, c);
       stretch = fmaxf(stretch, most);
       if (++in == per_mark || g + 1 == groups) {
         if (a.top) top.mark[mark][tid] = stretch;
@@ -336,61 +377,71 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobArgs a) {
         ++mark;
       }
     }
-    o.take<1>(&x0, x0, c);
+    o.template take<1>(&x0, x0, c);
     if (a.top) offer_lane(top, turn, tid < z.chunks || extra >= 0 ? (uint32_t)(rank_key(o.m, 0) >> 32) : 0);
-    o = over_workgroup(o, part[turn], c);
+    o = over_workgroup<OF / 64>(o, part[turn], c);
     const bool bad = o.sum != o.sum;
-    const auto find = [&]() {
-      return find_top(top, turn, a.top, [&](uint64_t bound, auto add) {
-        const float least = least_logit(bound);
-        if (extra >= 0 && rank_key(x0, (uint32_t)extra) >= bound) add(rank_key(x0, (uint32_t)extra));
-        for (int g = 0; g < groups; ++g) {
-          if (top.mark[g / per_mark][tid] < least) continue;
-          const int at = g * kThreads * kUnroll + tid;
-          if (groups > 1) load(at);         // (else still at hand)
-          uint32_t reach = 0;               // a bit for each element
+    // the classes of a chunk that reach the bound
+    const auto look = [&](const Bound& b, const uint4& chunk, int ch) {
+      float x[N];
+      unpack(chunk, x, (const T*)nullptr);
+      const int v = z.from + ch * N;
+      uint32_t reach = 0;
 #pragma unroll
-          for (int u = 0; u < kUnroll; ++u) {
-            float x[N];
-            unpack(raw[u], x, (const T*)nullptr);
+      for (int e = 0; e < N; ++e) reach |= (b.met(x[e], v) ? 1u : 0u) << e;
+      for (; reach; reach &= reach - 1) {
+        const int e = __builtin_ctz(reach);
+        float y = x[0];
 #pragma unroll
-            for (int e = 0; e < N; ++e) reach |= (x[e] >= least && at + u * kThreads < z.chunks ? 1u : 0u) << (u * N + e);
-          }
-          for (; reach; reach &= reach - 1) {
-            const int e = __builtin_ctz(reach), v = z.from + (at + e / N * kThreads) * N + e % N;
-            const uint64_t key = rank_key(as_float(z.z[v]), (uint32_t)v);
-            if (key >= bound) add(key);
-          }
-        }
-      });
+        for (int f = 1; f < N; ++f) y = e == f ? x[f] : y;
+        const uint64_t key = rank_key(y, (uint32_t)(v + e));
+        if (key >= b.key) add_found(top, turn, key);
+      }
+    };
+    const auto scan = [&](uint64_t bound) {
+      const Bound b(bound);
+      if (extra >= 0 && rank_key(x0, (uint32_t)extra) >= bound) add_found(top, turn, rank_key(x0, (uint32_t)extra));
+      if (z.chunks <= OF) {      // one a lane, still at hand
+        if (tid < z.chunks) look(b, first, tid);
+        return;
+      }
+      for (int mark = 0; mark * per_mark < groups; ++mark)
+        if (b.met(top.mark[mark][tid], (uint32_t)(z.from + (mark * per_mark * OF * kUnroll + tid) * N)))
+          top.stretch[atomicAdd(&top.stretches[turn], 1)] = (uint16_t)(mark * OF + tid);
+      __syncthreads();
+      const int each = per_mark * kUnroll, all = top.stretches[turn] * each;
+      for (int j = tid; j < all; j += OF) {
+        const int s = each == kUnroll ? j / kUnroll : j / each, at = top.stretch[s];
+        const int ch = at / OF * each * OF + at % OF + (j - s * each) * OF;
+        if (ch < z.chunks) look(b, z.body[ch], ch);
+        if (*(volatile int*)&top.count[turn] > TopLds<OF>::kCandidates) break;
+      }
     };
     if (PART) {
       if (tid == 0) a.parts[i] = o;
       if (!a.top) continue;
-      const int n = bad ? 0 : find();
-      uint64_t* const keys = a.keys + i * a.top;
-      for (int k = tid; k < n; k += kThreads) {
+      const int n = bad ? 0 : find_top(top, turn, a.top, scan);
+      uint64_t* const keys = a.keys + row * segs * a.top + seg;
+      for (int k = tid; k < n; k += OF) {
         const int r = rank_among(top.found, n, top.found[k]);
-        if (r < a.top) keys[r] = top.found[k];
+        if (r < a.top) keys[r * segs] = top.found[k];
       }
-      for (int k = n + tid; k < a.top; k += kThreads) keys[k] = 0;
+      for (int k = n + tid; k < a.top; k += OF) keys[k * segs] = 0;
     } else {
       answer.put(o);
-      if (a.top && !bad) {
-        const int n = find();
-        answer.put_top(top.found, n);
-      }
+      if (a.top && !bad) answer.put_top(top.found, find_top(top, turn, a.top, scan));
     }
   }
 }
 
+// The parts of rows joined.  Keys lie by rank, so that a lane's first one is among the greatest of its part.
 template <class T>
 __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) {
-  __shared__ TopLds top;
+  __shared__ TopLds<kThreads> top;
   const int tid = (int)threadIdx.x, n_keys = a.segs * a.top;
   int turn = 0;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-    RowAnswer<T> answer(a, row);
+    RowAnswer<T, kThreads> answer(a, row);
     const uint64_t* const keys = a.keys + row * n_keys;
     uint64_t mine = 0;
     for (int k = tid; k < n_keys; k += kThreads) mine = keys[k] > mine ? keys[k] : mine;
@@ -399,11 +450,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) 
     if (!a.top) continue;
     __syncthreads();
     if (answer.bad) continue;
-    const int n = find_top(top, turn, a.top, [&](uint64_t bound, auto add) {
-      for (int k = tid; k < n_keys; k += kThreads)
-        if (keys[k] && keys[k] >= bound) add(keys[k]);
-    });
-    answer.put_top(top.found, n);
+    const auto scan = [&](uint64_t bound) {
+      for (int k = tid; k < n_keys && mine >= bound; k += kThreads)
+        if (keys[k] && keys[k] >= bound) add_found(top, turn, keys[k]);
+    };
+    answer.put_top(top.found, find_top(top, turn, a.top, scan));
   }
 }
 
@@ -527,18 +578,17 @@ __device__ __forceinline__ void take_chunks(Sums<TWO>& o, const uint4* raw, floa
   o.template take<kOf * N>(x, most, c);
 }
 
-template <class T, bool TWO>
+template <class T, int OF, bool TWO>
 __device__ __forceinline__ Sums<TWO> sums_of(const RowSpan<T>& z, int extra, float c, Sums<TWO>* part) {
   Sums<TWO> o{-INFINITY, 0.0f, 0.0f};
   const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
-  for (int at = (int)threadIdx.x; at < z.chunks; at += kThreads * kUnroll) {
+  for (int at = (int)threadIdx.x; at < z.chunks; at += OF * kUnroll) {
     uint4 raw[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * kThreads < z.chunks ? z.body[at + u * kThreads] : all_minus_inf<T>();
+    load_chunks<OF>(z, at, raw);
     take_chunks<T, kUnroll>(o, raw, c);
   }
   o.template take<1>(&x0, x0, c);
-  return over_workgroup(o, part, c);
+  return over_workgroup<OF / 64>(o, part, c);
 }
 
 template <bool TWO>
@@ -587,15 +637,14 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, long long row, co
   if (threadIdx.x == 0) a.loss[row] = t.none ? 0.0f : loss;
 }
 
-// The class of the teacher's entry or of the label that this thread writes again at the end, and the gradient there, in full and rounded once.
+// The class of the teacher's entry or of the label (entry a.top) that a thread writes again at the end, and the gradient there, in full and rounded once.
 template <class T, bool TWO>
 struct Named {
   int at;                  // -1: none
   float value;
   template <class Here>
-  __device__ Named(const DistillArgs& a, const TeacherLds& l, const Terms<TWO>& t, int64_t label, Here here) {
-    const int tid = (int)threadIdx.x;
-    const int64_t id = tid < a.top ? l.id[tid] : tid == a.top ? label : -1;
+  __device__ Named(const DistillArgs& a, const TeacherLds& l, const Terms<TWO>& t, int64_t label, int entry, Here here) {
+    const int64_t id = entry < a.top ? l.id[entry] : entry == a.top ? label : -1;
     at = id >= 0 && !t.none && here(id) ? (int)id : -1;
     if (at < 0) return;
     float minus = 0.0f;
@@ -607,7 +656,7 @@ struct Named {
         minus += (ids.x == at ? q.x : 0.0f) + (ids.y == at ? q.y : 0.0f) + (ids.z == at ? q.z : 0.0f) + (ids.w == at ? q.w : 0.0f);
       }
     }
-    value = t.slope(tid < a.top ? l.z[tid] : l.z_label) - t.ct * minus - (t.labelled && at == label ? t.cl : 0.0f);
+    value = t.slope(entry < a.top ? l.z[entry] : l.z_label) - t.ct * minus - (t.labelled && at == label ? t.cl : 0.0f);
   }
   __device__ void put_into(T* g) const {
     if (at >= 0) put(g + at, value);
@@ -627,12 +676,12 @@ __device__ __forceinline__ uint4 slopes_of(const Terms<TWO>& t, const uint4& raw
 // the sums of parts of rows, where rows are shared out
 template <class T, bool TWO>
 __global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs a) {
-  __shared__ Sums<TWO> part[2][kWaves];
+  __shared__ Sums<TWO> part[2][kThreads / 64];
   int turn = 0;
   for (long long i = blockIdx.x; i < a.rows * a.segs; i += gridDim.x, turn ^= 1) {
     const long long row = i / a.segs;
     const RowSpan<T> z((const T*)a.logits + row * a.stride, a.classes, (int)(i - row * a.segs), a.segs);
-    const Sums<TWO> o = sums_of<T, TWO>(z, z.beside((int)threadIdx.x), first_factor(a), part[turn]);
+    const Sums<TWO> o = sums_of<T, kThreads>(z, z.beside((int)threadIdx.x), first_factor(a), part[turn]);
     if (threadIdx.x == 0) ((Sums<TWO>*)a.parts)[i] = o;
   }
 }
@@ -640,9 +689,9 @@ __global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs a) {
 // Loss and gradient of a row, or of one of `segs` parts of it.  One pass for the sums (none where the call brings them, or where a launch before
 // has formed those of parts), one that writes the gradient: for every class the probabilities' part; then the classes that the label or the teacher
 // names are written again.  TWO: both terms are there at different temperatures, that is two sums and two exponentials an element.
-template <class T, bool TWO>
-__global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
-  __shared__ Sums<TWO> part[kWaves];
+template <class T, bool TWO, int OF>
+__global__ __launch_bounds__(OF) void distill_kernel(DistillArgs a) {
+  __shared__ Sums<TWO> part[OF / 64];
   __shared__ TeacherLds teacher;
   constexpr int N = RowSpan<T>::kPer;
   const int tid = (int)threadIdx.x;
@@ -661,10 +710,10 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
     const auto load = [&](int at) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
-        if (at + u * kThreads < z.chunks) raw[u] = z.body[at + u * kThreads];
+        if (at + u * OF < z.chunks) raw[u] = z.body[at + u * OF];
     };
     const bool known = a.given_stats || a.n_parts;
-    if (!known) o = sums_of<T, TWO>(z, extra, c, part);
+    if (!known) o = sums_of<T, OF>(z, extra, c, part);
     if (a.grad) {          // on their way while the sums are joined and the teacher is waited for
       load(tid);
       if (extra >= 0) x0 = as_float(z.z[extra]);
@@ -681,14 +730,15 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
     if (a.loss && seg == 0 && tid < 64) put_loss(a, row, teacher, o, terms);
     if (a.grad) {
       T* const g = (T*)a.grad + row * a.grad_stride;
-      const Named<T, TWO> named(a, teacher, terms, label, [&](int64_t v) { return z.holds(v); });
+      const auto here = [&](int64_t v) { return z.holds(v); };
+      const Named<T, TWO> named(a, teacher, terms, label, tid, here);
       const bool same_phase = (((uintptr_t)g ^ (uintptr_t)z.z) & 15) == 0;
       if (extra >= 0) put(g + extra, terms.slope(x0));
-      for (int at = tid; at < z.chunks; at += kThreads * kUnroll) {
+      for (int at = tid; at < z.chunks; at += OF * kUnroll) {
         if (at != tid) load(at);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-          const int ch = at + u * kThreads;
+          const int ch = at + u * OF;
           if (ch >= z.chunks) continue;
           const uint4 v = slopes_of<T, TWO>(terms, raw[u]);
           T* const out = g + z.from + ch * N;
@@ -702,6 +752,7 @@ __global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a) {
       }
       __syncthreads();
       named.put_into(g);
+      for (int entry = OF + tid; entry <= a.top; entry += OF) Named<T, TWO>(a, teacher, terms, label, entry, here).put_into(g);     // (64 threads)
     }
     __syncthreads();       // (the next row's teacher takes the place of this one's)
   }
@@ -765,7 +816,8 @@ __global__ __launch_bounds__(OF, 4) void distill_held_kernel(DistillArgs a) {
     const Terms<TWO> terms(a, row, teacher, o, label, up);
     if (tid < 64) put_loss(a, row, teacher, o, terms);
     T* const g = (T*)a.grad + row * a.grad_stride;
-    const Named<T, TWO> named(a, teacher, terms, label, [&](int64_t v) { return v < a.classes; });
+    const auto here = [&](int64_t v) { return v < a.classes; };
+    const Named<T, TWO> named(a, teacher, terms, label, tid, here);
     if (const int extra = z.beside(tid); extra >= 0) put(g + extra, terms.slope(x0));
     const long long next = row + gridDim.x;
     const bool more = next < a.rows;
@@ -779,6 +831,7 @@ __global__ __launch_bounds__(OF, 4) void distill_held_kernel(DistillArgs a) {
     if (more) load_extra(zn);
     __syncthreads();
     named.put_into(g);
+    for (int entry = OF + tid; entry <= a.top; entry += OF) Named<T, TWO>(a, teacher, terms, label, entry, here).put_into(g);     // (64 threads)
     if (!more) return;
     row = next;
   }
@@ -825,52 +878,112 @@ int check_grad(const char* who, const void* grad, int32_t dtype, int64_t rows, i
   return CG_OK;
 }
 
-// Parts of a row: where there are few rows, as many as give a launch kEnough workgroups, of kUnroll chunks for a lane at least.
-constexpr int kEnough = 512, kPartBytes = kThreads * kUnroll * 16;
-int parts_of(int64_t rows, int64_t classes, int bytes) {
-  if (rows <= 0 || rows >= kEnough) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>((kEnough + rows - 1) / rows, (classes * bytes + kPartBytes - 1) / kPartBytes));
+// How rows are given to workgroups.  `chunks` are 16 bytes; 256 threads take kPart of them at once.
+constexpr int64_t kPart = kThreads * kUnroll;
+int64_t chunks_in(int64_t classes, int bytes) { return classes * bytes / 16; }
+
+// Parts of rows that are shared out, in a first launch for their sums and a second one that joins them: a few long rows, in parts of 16 KB and as many as
+// make `enough` workgroups, `fewest` at least.  One row of 131072 classes in bf16 with 20 alternatives 19.1 us whole, 10.8 us in 16 parts; 64 rows 20.4 and
+// 14.7 (8 parts), 128 rows 20.6 and 17.6 (4), 256 rows 21.2 and 23.3 (2); rows of 64 KB are never faster in parts (one row 8.7 and 11.1).  The loss alone, 32
+// teacher classes: 16 rows 11.0 and 7.8 us, 64 rows 12.2 and 11.1 (8 parts), 128 rows 12.8 and 14.0 (4).  Loss and gradient: one row 17.5 and 8.5,
+// 64 rows 21.3 and 16.7, 128 rows 24.0 and 23.3 (8 parts), 192 rows 27.3 and 34.3.
+constexpr int kEnough = 512;
+int parts_of(int64_t rows, int64_t chunks, int enough, int fewest) {
+  if (rows <= 0 || enough / rows < fewest || chunks <= 4 * kPart) return 1;
+  return (int)std::min<int64_t>(enough / rows, (chunks + kPart - 1) / kPart);
 }
+int logprob_parts(int64_t rows, int64_t chunks) { return parts_of(rows, chunks, kEnough, 4); }
+int distill_parts(int64_t rows, int64_t chunks, bool grad) { return parts_of(rows, chunks, grad ? 2 * kEnough : kEnough, 8); }
+
+// Many short rows: a wavefront each, while 256 threads had too little to do between their barriers.  Alternatives: 4096 rows of 2048 classes in bf16 11.3 us, by
+// workgroups of 256 threads 25.5 us; 1024 rows of 4096 8.1 and 9.0, of 8192 10.7 and 10.2; 256 rows of 2048 6.7 and 6.4.  The loss alone: 4096 rows of 1000 7.7 and
+// 16.8 us, of 8192 17.3 and 21.6; 512 rows of 4096 5.3 and 5.4, of 8192 6.4 and 5.4.
+bool wavefront_each(int64_t rows, int64_t chunks) { return rows >= 512 && chunks <= std::min<int64_t>(rows / 2, 1024); }
 
 template <class T>
 void launch_logprobs(const LogprobArgs& a, hipStream_t s) {
   if (a.segs > 1) {
-    hipLaunchKernelGGL((logprobs_kernel<T, true>), dim3((unsigned)(a.rows * a.segs)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((logprobs_kernel<T, true, 256>), dim3((unsigned)(a.rows * a.segs)), dim3(256), 0, s, a);
     hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, a);
+  } else if (wavefront_each(a.rows, chunks_in(a.classes, sizeof(T))) && a.top <= 32) {       // (a bound from 64 lanes)
+    hipLaunchKernelGGL((logprobs_kernel<T, false, 64>), dim3(row_groups(a.rows)), dim3(64), 0, s, a);
   } else {
-    hipLaunchKernelGGL((logprobs_kernel<T, false>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((logprobs_kernel<T, false, 256>), dim3(row_groups(a.rows)), dim3(256), 0, s, a);
   }
+}
+
+// Threads of distill_held_kernel for a row: as few as hold it, and more as long as all of them find room at once (1024 threads on each of 256 compute
+// units) and each has four chunks.  32768 classes in bf16: 64 rows 9.6 us on 256 threads, 8.1 on 512, 8.0 on 1024, 512 rows 18.9, 18.0 and 19.3,
+// 1024 rows 32.8, 33.5 and 38.5; 4096 rows of 1000 in fp32 12.1 us on 64 threads and 21.8 on 256.
+constexpr int64_t kRoom = 256 * 1024;
+int held_threads(int64_t rows, int64_t chunks) {
+  int of = 64;
+  while (of < 1024) {
+    const int more = of == 64 ? 256 : of * 2;
+    if (chunks <= kHeld * of && (rows * more > kRoom || chunks < 4 * more)) break;
+    of = more;
+  }
+  return of;
+}
+
+template <class T, bool TWO>
+void launch_held(const DistillArgs& a, int64_t chunks, hipStream_t s) {
+  const int of = held_threads(a.rows, chunks);
+  const dim3 grid((unsigned)std::min<int64_t>(a.rows, kRoom / of));
+  if (of == 64)
+    hipLaunchKernelGGL((distill_held_kernel<T, TWO, 64>), grid, dim3(64), 0, s, a);
+  else if (of == 256)
+    hipLaunchKernelGGL((distill_held_kernel<T, TWO, 256>), grid, dim3(256), 0, s, a);
+  else if (of == 512)
+    hipLaunchKernelGGL((distill_held_kernel<T, TWO, 512>), grid, dim3(512), 0, s, a);
+  else
+    hipLaunchKernelGGL((distill_held_kernel<T, TWO, 1024>), grid, dim3(1024), 0, s, a);
+}
+
+// a.segs parts a row by workgroups of 256 threads; whole rows also by wavefronts, and long ones that do not fill the compute units by 512 threads (256 rows of
+// 131072 classes in bf16, the loss alone, 14.4 us and 19.2 on 256; 128 rows of 32768 5.8 and 8.0; 512 rows of 32768 10.6 and 10.6, 768 rows 15.5 and 12.8).
+template <class T, bool TWO>
+void launch_rows_of(const DistillArgs& a, int64_t chunks, hipStream_t s) {
+  const dim3 grid(row_groups(a.rows * a.segs));
+  if (a.segs == 1 && wavefront_each(a.rows, chunks))
+    hipLaunchKernelGGL((distill_kernel<T, TWO, 64>), grid, dim3(64), 0, s, a);
+  else if (a.segs == 1 && !a.n_parts && a.rows <= 256 && chunks >= 2 * kPart)
+    hipLaunchKernelGGL((distill_kernel<T, TWO, 512>), grid, dim3(512), 0, s, a);
+  else
+    hipLaunchKernelGGL((distill_kernel<T, TWO, 256>), grid, dim3(256), 0, s, a);
 }
 
 template <class T, bool TWO>
 void launch_distill_as(DistillArgs a, hipStream_t s) {
-  const int segs = parts_of(a.rows, a.classes, sizeof(T));
-  a.segs = segs;
-  const int64_t chunks = ((int64_t)a.classes * (int)sizeof(T)) / 16;
-  const bool same_phase = (((uintptr_t)a.grad ^ (uintptr_t)a.logits) & 15) == 0 && (a.rows == 1 || (a.grad_stride - a.stride) * (int)sizeof(T) % 16 == 0);
-  if (segs == 1 && a.grad && !a.given_stats && chunks <= kHeld * 1024 && same_phase) {
-    // workgroups that a compute unit's registers hold at once: 1024 threads on each of 256
-    if (chunks <= kHeld * 256)
-      hipLaunchKernelGGL((distill_held_kernel<T, TWO, 256>), dim3((unsigned)std::min<int64_t>(a.rows, 1024)), dim3(256), 0, s, a);
-    else if (chunks <= kHeld * 512)
-      hipLaunchKernelGGL((distill_held_kernel<T, TWO, 512>), dim3((unsigned)std::min<int64_t>(a.rows, 512)), dim3(512), 0, s, a);
-    else
-      hipLaunchKernelGGL((distill_held_kernel<T, TWO, 1024>), dim3((unsigned)std::min<int64_t>(a.rows, 256)), dim3(1024), 0, s, a);
+  const int64_t chunks = chunks_in(a.classes, sizeof(T));
+  if (a.given_stats) {
+    // The gradient alone, in parts of 32 KB (16 KB where those are few): 1024 rows of 131072 classes in bf16 105.5 us, by whole rows 117.9; 64 rows 10.7 and 22.9.
+    const int64_t parts = std::max<int64_t>(1, chunks / (2 * kPart));
+    a.segs = (int)(a.rows * parts < kEnough ? std::max<int64_t>(1, chunks / kPart) : parts);
+    launch_rows_of<T, TWO>(a, chunks, s);
     return;
   }
-  if (segs > 1 && !a.given_stats) {
+  const bool same_phase = (((uintptr_t)a.grad ^ (uintptr_t)a.logits) & 15) == 0 && (a.rows == 1 || (a.grad_stride - a.stride) * (int)sizeof(T) % 16 == 0);
+  const int segs = distill_parts(a.rows, chunks, a.grad != nullptr);
+  if (segs > 1) {
+    a.segs = segs;
     hipLaunchKernelGGL((distill_part_kernel<T, TWO>), dim3((unsigned)(a.rows * segs)), dim3(kThreads), 0, s, a);
     a.n_parts = segs;
-    if (a.grad == a.logits) {      // the loss asks for logits that another part's workgroup replaces by their gradient: it goes first
+    if (!a.grad) {
+      a.segs = 1;
+    } else if (a.grad == a.logits) {      // the loss asks for logits that another part's workgroup replaces by their gradient: it goes first
       DistillArgs first = a;
       first.grad = nullptr;
       first.segs = 1;
-      hipLaunchKernelGGL((distill_kernel<T, TWO>), dim3(row_groups(a.rows)), dim3(kThreads), 0, s, first);
+      launch_rows_of<T, TWO>(first, chunks, s);
       a.loss = nullptr;
     }
-    if (!a.grad) a.segs = 1;
+    launch_rows_of<T, TWO>(a, chunks, s);
+  } else if (a.grad && chunks <= kHeld * 1024 && same_phase) {
+    launch_held<T, TWO>(a, chunks, s);
+  } else {
+    launch_rows_of<T, TWO>(a, chunks, s);
   }
-  hipLaunchKernelGGL((distill_kernel<T, TWO>), dim3(row_groups(a.rows * a.segs)), dim3(kThreads), 0, s, a);
 }
 
 template <class T>
@@ -897,9 +1010,8 @@ extern "C" {
 
 size_t cg_logprobs_workspace_bytes(int64_t rows, int32_t classes, int32_t top) {
   if (rows <= 0 || classes <= 0 || top < 0 || top > CG_TOP_MAX) return 0;
-  // (the larger of the two types' needs)
-  const int segs = parts_of(rows, classes, 4);
-  return segs == 1 ? 0 : (size_t)rows * segs * (sizeof(Online) + 8 + 8 * (size_t)top);
+  const int segs = logprob_parts(rows, chunks_in(classes, 4));      // (the larger of the two types' needs)
+  return segs == 1 ? 0 : (size_t)rows * segs * (sizeof(Online) + 8 * (size_t)top);
 }
 
 int cg_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t classes, int64_t row_stride, float temperature, const int64_t* labels,
@@ -918,7 +1030,7 @@ int cg_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t classes
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256)))
     return cg::set_error(CG_EINVAL, "%s: needs %zu bytes of workspace, 256-byte aligned", who, need);
   LogprobArgs a{logits, rows, row_stride, classes, given, top, 1, 1.0f / temperature, labels, logprob, entropy, top_ids, top_logprobs, nullptr, nullptr};
-  a.segs = parts_of(rows, classes, element_bytes(dtype));
+  a.segs = logprob_parts(rows, chunks_in(classes, element_bytes(dtype)));
   if (a.segs > 1) {
     a.keys = (uint64_t*)workspace;
     a.parts = (Online*)(a.keys + rows * a.segs * top);
@@ -934,7 +1046,7 @@ int cg_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t classes
 
 size_t cg_distill_workspace_bytes(int64_t rows, int32_t classes) {
   if (rows <= 0 || classes <= 0) return 0;
-  const int segs = parts_of(rows, classes, 4);      // (the larger of the two types' needs)
+  const int segs = std::max(distill_parts(rows, chunks_in(classes, 4), false), distill_parts(rows, chunks_in(classes, 4), true));      // (fp32: the larger need)
   return segs == 1 ? 0 : (size_t)rows * segs * 3 * sizeof(float);
 }
 
