@@ -105,11 +105,23 @@ __device__ __forceinline__ float sum_over_lanes(float x) {
   return over_lanes(x, [](float a, float b) { return a + b; });
 }
 
-// the chunks at, at + OF, ... of a part; -inf where it has none
-template <int OF, class T>
-__device__ __forceinline__ void load_chunks(const RowSpan<T>& z, int at, uint4 (&raw)[kUnroll]) {
+// `count` chunks, at most 2^27, as a buffer: what lies behind them is neither read nor written, and no access needs a branch or registers for an address
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk_buffer(const void* at, int count) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)at, (short)0, count * 16, 0x00027000);
+}
+
+// the next OF * kOf chunks of a part from chunk `first` on; -inf where it has none
+template <int OF, class T, int kOf>
+__device__ __forceinline__ void load_chunks(const RowSpan<T>& z, int first, uint4 (&raw)[kOf]) {
+  const int left = z.chunks - first, tid = (int)threadIdx.x;
+  const __amdgpu_buffer_rsrc_t from = chunk_buffer(z.body + first, left < OF * kOf ? left : OF * kOf);
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) raw[u] = at + u * OF < z.chunks ? z.body[at + u * OF] : all_minus_inf<T>();
+  for (int u = 0; u < kOf; ++u) raw[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, (tid + u * OF) * 16, 0, 0));
+  if (left < OF * kOf) {
+#pragma unroll
+    for (int u = 0; u < kOf; ++u)
+      if (tid + u * OF >= left) raw[u] = all_minus_inf<T>();
+  }
 }
 
 // A softmax in one pass: with m the greatest logit so far, the sum of e = 2^((z - m) c) and the sum of e (z - m) c, c = log2(e) / temperature.
@@ -359,13 +371,13 @@ __global__ __launch_bounds__(OF) void logprobs_kernel(LogprobArgs a) {
     const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
     float stretch = -INFINITY;
     uint4 raw[kUnroll], first;
-    load_chunks<OF>(z, tid, raw);
+    load_chunks<OF>(z, 0, raw);
     first = raw[0];
     for (int g = 0, in = 0, mark = 0; g < groups; ++g) {
       float x[kUnroll * N], most = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) unpack(raw[u], x + u * N, (const T*)nullptr);
-      if (g + 1 < groups) load_chunks<OF>(z, (g + 1) * OF * kUnroll + tid, raw);      // on their way meanwhile
+      if (g + 1 < groups) load_chunks<OF>(z, (g + 1) * OF * kUnroll, raw);      // on their way meanwhile
 #pragma unroll
       for (int e = 0; e < kUnroll * N; ++e) most = fmaxf(most, x[e]);
       o.template take<kUnroll * N>(x, most, c);
@@ -582,9 +594,9 @@ template <class T, int OF, bool TWO>
 __device__ __forceinline__ Sums<TWO> sums_of(const RowSpan<T>& z, int extra, float c, Sums<TWO>* part) {
   Sums<TWO> o{-INFINITY, 0.0f, 0.0f};
   const float x0 = extra >= 0 ? as_float(z.z[extra]) : -INFINITY;
-  for (int at = (int)threadIdx.x; at < z.chunks; at += OF * kUnroll) {
+  for (int first = 0; first < z.chunks; first += OF * kUnroll) {
     uint4 raw[kUnroll];
-    load_chunks<OF>(z, at, raw);
+    load_chunks<OF>(z, first, raw);
     take_chunks<T, kUnroll>(o, raw, c);
   }
   o.template take<1>(&x0, x0, c);
@@ -758,11 +770,12 @@ __global__ __launch_bounds__(OF) void distill_kernel(DistillArgs a) {
   }
 }
 
-// Loss and gradient of rows of up to kHeld * OF chunks in one pass: a row stays in the registers of its workgroup between its sums and its gradient, and as
-// the gradient leaves, the next row's chunks take the registers' place, so that loads and stores are on their way together.  A workgroup walks rows.
-// Rows of logits and gradient have the same alignment to 16 bytes.  Chunks are accessed through buffers of their number: what lies behind the last one
-// is neither read nor written, and no access needs registers for an address.
-constexpr int kHeld = 16;
+// Loss and gradient in one pass: kHeld chunks a lane stay in the registers of the row's workgroup between the sums and the gradient (256 KB by 1024 threads, half of
+// a compute unit's registers), and as the gradient leaves, the next row's chunks take their place, so that loads and stores are on their way together.  A
+// workgroup walks rows.  What a longer row has beside (1024 threads only) is read twice.  Rows of logits and gradient have the same alignment to 16 bytes.
+// Bound by memory: 4096 rows of 131072 classes in bf16 461 us, 4.66 TB/s of one read and one write an element, where a plain copy reaches 4.83; read
+// twice by distill_kernel they took 647 us.  2048 rows of 131072 in fp32 (twice what is held) 494 and 648 us, of 200003 839 and 1103 us.
+constexpr int kHeld = 16, kMore = 2;       // kMore: chunks a lane takes at once of what is beside
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <class T, bool TWO, int OF>
@@ -776,7 +789,7 @@ __global__ __launch_bounds__(OF, 4) void distill_held_kernel(DistillArgs a) {
   float x0 = 0.0f;
   int turn = 0;
   const auto row_at = [&](long long row) { return RowSpan<T>((const T*)a.logits + row * a.stride, a.classes, 0, 1); };
-  const auto chunks_of = [](const void* body, int chunks) { return __builtin_amdgcn_make_buffer_rsrc((void*)body, (short)0, chunks * 16, 0x00027000); };
+  const auto held = [](const RowSpan<T>& z) { return z.chunks < kHeld * OF ? z.chunks : kHeld * OF; };
   const auto load = [&](__amdgpu_buffer_rsrc_t from, int u) {
     raw[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, (tid + u * OF) * 16, 0, 0));
   };
@@ -787,7 +800,7 @@ __global__ __launch_bounds__(OF, 4) void distill_held_kernel(DistillArgs a) {
   long long row = blockIdx.x;
   {
     const RowSpan<T> z = row_at(row);
-    const __amdgpu_buffer_rsrc_t from = chunks_of(z.body, z.chunks);
+    const __amdgpu_buffer_rsrc_t from = chunk_buffer(z.body, held(z));
 #pragma unroll
     for (int u = 0; u < kHeld; ++u)
       if (u * OF < z.chunks) load(from, u);
@@ -810,6 +823,14 @@ __global__ __launch_bounds__(OF, 4) void distill_held_kernel(DistillArgs a) {
       }
       take_chunks<T, kTake>(o, raw + u, c);
     }
+    if (OF == 1024) {        // what a longer row has beside, a second time below
+#pragma unroll 1
+      for (int first = kHeld * OF; first < z.chunks; first += OF * kMore) {
+        uint4 some[kMore];
+        load_chunks<OF>(z, first, some);
+        take_chunks<T, kMore>(o, some, c);
+      }
+    }
     o.template take<1>(&x0, x0, c);
     o = over_workgroup<OF / 64>(o, part[turn], c);
     if (a.stats && tid == 0) put_stats(a, row, o);
@@ -819,10 +840,21 @@ __global__ __launch_bounds__(OF, 4) void distill_held_kernel(DistillArgs a) {
     const auto here = [&](int64_t v) { return v < a.classes; };
     const Named<T, TWO> named(a, teacher, terms, label, tid, here);
     if (const int extra = z.beside(tid); extra >= 0) put(g + extra, terms.slope(x0));
+    if (OF == 1024) {
+#pragma unroll 1
+      for (int first = kHeld * OF; first < z.chunks; first += OF * kMore) {
+        uint4 some[kMore];
+        load_chunks<OF>(z, first, some);
+        const __amdgpu_buffer_rsrc_t to = chunk_buffer(g + z.from + (long long)first * RowSpan<T>::kPer, z.chunks - first < OF * kMore ? z.chunks - first : OF * kMore);
+#pragma unroll
+        for (int u = 0; u < kMore; ++u)
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, slopes_of<T, TWO>(terms, some[u])), to, (tid + u * OF) * 16, 0, 0);
+      }
+    }
     const long long next = row + gridDim.x;
     const bool more = next < a.rows;
     const RowSpan<T> zn = row_at(more ? next : row);
-    const __amdgpu_buffer_rsrc_t to = chunks_of(g + z.from, z.chunks), from = chunks_of(zn.body, more ? zn.chunks : 0);
+    const __amdgpu_buffer_rsrc_t to = chunk_buffer(g + z.from, held(z)), from = chunk_buffer(zn.body, more ? held(zn) : 0);
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) {
       if (u * OF < z.chunks) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, slopes_of<T, TWO>(terms, raw[u])), to, (tid + u * OF) * 16, 0, 0);
@@ -979,7 +1011,7 @@ void launch_distill_as(DistillArgs a, hipStream_t s) {
       a.loss = nullptr;
     }
     launch_rows_of<T, TWO>(a, chunks, s);
-  } else if (a.grad && chunks <= kHeld * 1024 && same_phase) {
+  } else if (a.grad && same_phase) {
     launch_held<T, TWO>(a, chunks, s);
   } else {
     launch_rows_of<T, TWO>(a, chunks, s);
