@@ -260,6 +260,12 @@ class GatedResNet18:
             trace["fc"] = dict(x=cur, y=logits)
         return logits
 
+    def answers(self, x, labels=None, top: int = 5):
+        """The network's answers to a batch: (logits, logprob, entropy, top_ids, top_logprobs), the last four as binding.logprobs gives them (log
+        probabilities of the labels, entropies, the `top` likeliest classes).  What a teacher hands to binding.distill."""
+        logits = self.forward(x)
+        return (logits, *B.logprobs(logits, labels, top=min(top, self.classes)))
+
     def close(self):
         for layer in list(self.layers) + list(self.shortcuts.values()):
             if layer is not None:
@@ -276,6 +282,7 @@ def main():
     args = ap.parse_args()
     torch.cuda.set_device(0)
     out = {}
+    student = None
     for tag, rho in (("gated", args.rho), ("dense", 0.0)):
         net = GatedResNet18(max(args.batch, 4), args.size, rho=rho, grouped=args.grouped and rho > 0)    # (calibrates on four)
         rng = np.random.default_rng(1)
@@ -313,7 +320,13 @@ def main():
                 tot += int(c[0]) | (int(c[1]) << 32)
                 act += tr[spec.name]["y"].numel()
             fired = tot / act
-        out[tag] = dict(images_per_s=round(args.batch / dt, 1), ms_per_batch=round(dt * 1e3, 3), fired=fired)
+        logits, _, entropy, top_ids, top_logprobs = net.answers(x, top=16)
+        out[tag] = dict(images_per_s=round(args.batch / dt, 1), ms_per_batch=round(dt * 1e3, 3), fired=fired,
+                        entropy=round(entropy.mean().item(), 4), top_1=round(top_logprobs[:, 0].exp().mean().item(), 4))
+        if student is None:
+            student = logits
+        else:               # what distilling the dense network's answers into the gated one would start from (the two have weights of their own)
+            out["distillation_loss"] = round(B.distill(student, top_ids, top_logprobs)[0].mean().item(), 4)
         net.close()
     print(json.dumps(dict(network="ResNet-18, %dx%d, batch %d, bf16, random weights, synthetic images" %
                           (args.size, args.size, args.batch), **out)))
