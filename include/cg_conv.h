@@ -253,7 +253,7 @@ int cg_avgpool_fc(const void* x, const void* wfc, const float* bias, float* logi
  */
 enum { CG_TOP_MAX = 128 }; /* the most alternatives, and the most classes of a teacher, per row */
 
-/* Log probabilities log p = log softmax(logits / temperature), temperature > 0:
+/* Log probabilities log p = log softmax(logits / temperature), temperature between 2^-126 and 2^126:
  *   logprob       [rows][given]: those of the classes labels[rows][given].  A negative label is absent: 0; one of `classes`
  *                 or more gives NaN.  Not touched if given == 0 (both nullable then).
  *   entropy       nullable, [rows]: -sum p log p

@@ -418,7 +418,7 @@ __global__ __launch_bounds__(OF) void logprobs_kernel(LogprobArgs a) {
         return;
       }
       for (int mark = 0; mark * per_mark < groups; ++mark)
-        if (b.met(top.mark[mark][tid], (uint32_t)(z.from + (mark * per_mark * OF * kUnroll + tid) * N)))
+        if (b.met(top.mark[mark][tid], (uint32_t)z.from + (uint32_t)(mark * per_mark * OF * kUnroll + tid) * N))
           top.stretch[atomicAdd(&top.stretches[turn], 1)] = (uint16_t)(mark * OF + tid);
       __syncthreads();
       const int each = per_mark * kUnroll, all = top.stretches[turn] * each;
@@ -878,8 +878,8 @@ int check_logits(const char* who, const void* logits, int32_t dtype, int64_t row
   if (rows < 0 || classes <= 0) return cg::set_error(CG_EINVAL, "%s: bad size", who);
   if (dtype != CG_F32 && dtype != CG_BF16) return cg::set_error(CG_EUNSUPPORTED, "%s: logits are CG_F32 or CG_BF16", who);
   if (row_stride < 0) return cg::set_error(CG_EINVAL, "%s: row_stride must not be negative", who);
-  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-    return cg::set_error(CG_EINVAL, "%s: temperature must be positive and finite, and its inverse too", who);
+  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isnormal(1.0f / temperature) || !std::isfinite(1.0f / temperature * kLog2E))
+    return cg::set_error(CG_EINVAL, "%s: temperature must be positive and lie between 2^-126 and 2^126", who);
   if (rows > 0 && row_stride > (int64_t)((1ull << 62) / (uint64_t)rows)) return cg::set_error(CG_EINVAL, "%s: bad size", who);
   if (rows > 0 && !logits) return cg::set_error(CG_EINVAL, "%s: logits must not be NULL", who);
   if (!aligned(logits, element_bytes(dtype))) return cg::set_error(CG_EINVAL, "%s: logits must be aligned to their elements", who);

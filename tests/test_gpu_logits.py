@@ -121,6 +121,51 @@ def test_logprobs_where_one_lane_holds_the_alternatives(classes):
     check_logprobs(z, None, 128)
 
 
+@pytest.mark.parametrize("classes", [9, 1000])
+@pytest.mark.parametrize("top", [9, 32, 33])
+def test_logprobs_of_special_rows_among_many(classes, top):
+    """Short rows in great numbers: NaN, infinities, ties and masks beside each other."""
+    rng = np.random.default_rng(top)
+    z = rows_of(rng, 8, classes, "f32")
+    z[0] = -INF
+    z[1, 1:] = -INF
+    z[2, 3] = NAN
+    z[3, classes - 1] = INF
+    z[4] = 1.5
+    z[5] = torch.finfo(torch.float32).min
+    z[6] = torch.arange(classes, device="cuda") % 3
+    many = z.repeat(100, 1)
+    labels = rng.integers(-1, classes + 1, 800)
+    labels[:8] = 0
+    got = check_logprobs(many, labels, min(top, classes), given_rows=range(40))
+    for t in got[1:]:
+        assert same_bits(t, t[:8].repeat(100, *[1] * (t.dim() - 1)))
+
+
+def test_one_row_of_two_to_the_31_less_one_classes():
+    """The longest row: zeros but for a few classes, so that every value is known."""
+    classes = 2 ** 31 - 1
+    z = torch.zeros((1, classes), dtype=torch.bfloat16, device="cuda")
+    at = [0, 7, 2 ** 30, classes - 2, classes - 1]
+    z[0, at] = torch.tensor([20.0, 21.0, 22.0, 23.0, 24.0], dtype=torch.bfloat16, device="cuda")
+    total = classes - 5 + sum(np.exp(v) for v in (20.0, 21.0, 22.0, 23.0, 24.0))
+    label = torch.tensor([classes - 2], device="cuda")
+    logprob, entropy, ids, alternatives = B.logprobs(z, label, top=7)
+    assert ids[0].tolist() == at[::-1] + [1, 2]
+    want = np.array([24.0, 23.0, 22.0, 21.0, 20.0, 0.0, 0.0]) - np.log(total)
+    # (sums of whole numbers below 2^24 are exact; the five exponentials and each sum of parts round)
+    assert np.abs(alternatives[0].cpu().numpy() - want).max() <= 200 * O.U * 24 and abs(logprob.item() - want[1]) <= 200 * O.U * 24
+    t = torch.tensor([[1.0, 0.0]], device="cuda")
+    ids = torch.tensor([[classes - 1, 5]], device="cuda")
+    q = 1 / (1 + np.exp(-1.0))
+    loss, stats, grad = B.distill(z, ids, t, label, label_weight=1.0, grad=True)
+    assert abs(loss.item() - (q * (np.log(q) - want[0]) + (1 - q) * (np.log(1 - q) - want[6]) - want[1])) <= 600 * O.U * 24
+    step = 2.0 ** -8 + 1e-5
+    for v, x in ((0, 2 * np.exp(20) / total), (classes - 2, 2 * np.exp(23) / total - 1), (classes - 1, 2 * np.exp(24) / total - q), (5, 2 / total - (1 - q)),
+                 (2 ** 31 - 100, 2 / total)):
+        assert abs(grad[0, v].item() - x) <= step * abs(x) + 1e-5 * (v in (5, classes - 1, classes - 2)), v
+
+
 def test_logprobs_leave_out_what_is_not_asked_for():
     z = rows_of(np.random.default_rng(1), 4, 777, "f32")
     assert [o is None for o in B.logprobs(z, entropy=False)] == [True] * 4
@@ -248,6 +293,19 @@ def test_distill_of_many_rows(rows):
                       given_rows=range(0, rows, 1 + rows // 20))
 
 
+@pytest.mark.parametrize("rows,classes,dtype,top", [(4200, 100, "f32", 7), (700, 300, "f32", 100), (1500, 4100, "f32", 16), (600, 12001, "f32", 128),
+                                                    (300, 70001, "bf16", 33), (300, 140001, "bf16", 40), (130, 70001, "f32", 20), (129, 66000, "f32", 3)])
+def test_distill_of_rows_walked_in_turn(rows, classes, dtype, top):
+    """More rows than there are workgroups, of every length that registers hold and longer ones; in place as well."""
+    rng = np.random.default_rng(rows)
+    z = rows_of(rng, rows, classes, dtype)
+    ids = rng.integers(0, classes, (rows, top))
+    ids[rng.random((rows, top)) < 0.1] = -1
+    labels = rng.integers(-1, classes, rows)
+    check_distill(z, ids, (3 * rng.standard_normal((rows, top))).astype(np.float32), labels, 0.5, 0.5, (1.0, 2.0)[rows % 2],
+                  rng.standard_normal(rows).astype(np.float32), given_rows=[0, 1, rows // 2, rows - 2, rows - 1], in_place=True)
+
+
 def special_rows(rng, classes, dtype):
     z = rows_of(rng, 20, classes, dtype)
     ids, t, labels = teacher_of(rng, 20, classes, 8)
@@ -285,6 +343,14 @@ def special_rows(rng, classes, dtype):
 @pytest.mark.parametrize("wt,wl,temperature", [(0.5, 0.5, 1.0), (4.0, 0.5, 2.0), (1.0, 0.0, 0.7), (0.0, 1.0, 1.0)])
 def test_distill_of_special_rows(classes, wt, wl, temperature, dtype):
     check_distill(*special_rows(np.random.default_rng(classes), classes, dtype), wt, wl, temperature, in_place=True)
+
+
+@pytest.mark.parametrize("classes", [9, 1000])
+def test_distill_of_special_rows_among_many(classes):
+    z, ids, t, labels = special_rows(np.random.default_rng(classes), classes, "f32")
+    again = lambda a: np.tile(a, (30,) + (1,) * (a.ndim - 1))  # noqa: E731
+    loss, grad = check_distill(z.repeat(30, 1), again(ids), again(t), again(labels), 0.5, 0.5, 2.0, given_rows=range(20), in_place=True)
+    assert same_bits(loss, loss[:20].repeat(30)) and same_bits(grad, grad[:20].repeat(30, 1))
 
 
 def test_distill_gradient_is_the_loss_difference():
@@ -417,6 +483,16 @@ def test_with_and_without_the_calls_extension(monkeypatch):
     monkeypatch.setattr(B, "_calls", None)
     for w, g in zip(want, every()):
         assert w.shape == g.shape and w.stride() == g.stride() and w.dtype == g.dtype and same_bits(w, g)
+    # the small outputs of a call share a block of memory and nothing else
+    monkeypatch.setattr(B, "_calls", calls)
+    with torch.inference_mode():
+        assert all(o.is_inference() for o in B.logprobs(z, labels, top=7))
+    outs = [*B.logprobs(z, labels, top=7), *B.distill(z, ids, t)[:2]]
+    copies = [o.clone() for o in outs]
+    for o, c in zip(outs, copies):
+        o.fill_(3)
+        assert all(same_bits(x, y) or x is o for x, y in zip(outs, copies))
+        o.copy_(c)
     # what the extension leaves to Python
     assert calls.logprobs(z, labels, 2000, 1.0, True) is None and calls.logprobs(z.half(), None, 0, 1.0, True) is None
     assert calls.logprobs(z, labels.int(), 0, 1.0, True) is None and calls.logprobs(z.t(), None, 0, 1.0, True) is None

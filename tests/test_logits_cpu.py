@@ -33,7 +33,7 @@ def backward_args(**kw):
 LOGITS = [(dict(dtype=B.CG_I8), B.CG_EUNSUPPORTED), (dict(dtype=7), B.CG_EUNSUPPORTED), (dict(rows=-1), B.CG_EINVAL), (dict(classes=0), B.CG_EINVAL),
           (dict(classes=-3), B.CG_EINVAL), (dict(row_stride=-1), B.CG_EINVAL), (dict(row_stride=1 << 61), B.CG_EINVAL), (dict(temperature=0.0), B.CG_EINVAL),
           (dict(temperature=-1.0), B.CG_EINVAL), (dict(temperature=float("inf")), B.CG_EINVAL), (dict(temperature=float("nan")), B.CG_EINVAL),
-          (dict(temperature=1e-42), B.CG_EINVAL), (dict(logits=0), B.CG_EINVAL), (dict(logits=P + 2), B.CG_EINVAL),
+          (dict(temperature=1e-42), B.CG_EINVAL), (dict(temperature=3.1e-39), B.CG_EINVAL), (dict(temperature=3e38), B.CG_EINVAL), (dict(logits=0), B.CG_EINVAL), (dict(logits=P + 2), B.CG_EINVAL),
           (dict(logits=P + 1, dtype=B.CG_BF16), B.CG_EINVAL)]
 TEACHER = [(dict(top=-1), B.CG_EINVAL), (dict(top=129), B.CG_EUNSUPPORTED), (dict(top=0), B.CG_EINVAL), (dict(top_ids=0), B.CG_EINVAL),
            (dict(top_logits=0), B.CG_EINVAL), (dict(labels=0), B.CG_EINVAL), (dict(teacher_weight=float("nan")), B.CG_EINVAL),
