@@ -244,10 +244,28 @@ __device__ __forceinline__ void add_found(TopLds<OF>& l, int turn, uint64_t key)
   if (at < TopLds<OF>::kCandidates) l.found[at] = key;
 }
 
-// The `top` greatest keys of a workgroup's lanes, which are all different: found[0, n) holds them, and few others.  scan(bound) calls add_found for
-// every key from `bound` up, or for more than kCandidates of them.  The top-th of the lanes' greatest keys, cut to 16 bits, is a bound that at least
-// `top` keys reach; as a rule few more do.  Where `found` does not hold them (equal logits, or a lane that has many of the greatest), the same is done
-// with those that it took, whichever these are: the bound then rises above OF - top of them at least.
+// The top-th of the lanes' greatest among found[0, n), more than OF keys: at least `top` of them reach it, and those of OF - top lanes do not.
+template <int OF>
+__device__ __forceinline__ uint64_t raised_bound(const TopLds<OF>& l, int n, int top) {
+  uint32_t upper[OF / 64], lower[OF / 64];
+#pragma unroll
+  for (int w = 0; w < OF / 64; ++w) {
+    uint64_t most = 0;
+    for (int i = w * 64 + ((int)threadIdx.x & 63); i < n; i += OF) most = l.found[i] > most ? l.found[i] : most;
+    upper[w] = (uint32_t)(most >> 32);
+    lower[w] = (uint32_t)most;
+  }
+  const uint32_t u = reached_by<32, 32>(upper, top);
+#pragma unroll
+  for (int w = 0; w < OF / 64; ++w) lower[w] = upper[w] > u ? ~0u : upper[w] == u ? lower[w] : 0;
+  return (uint64_t)u << 32 | reached_by<32, 32>(lower, top);
+}
+
+// The `top` < OF greatest keys of a workgroup's lanes, which are all different: found[0, n) holds them, and few others, at most OF in all.  scan(bound) calls
+// add_found for every key from `bound` up, or for more than kCandidates of them.  The top-th of the lanes' greatest keys, cut to 16 bits, is a bound that
+// at least `top` keys reach; as a rule few more do.  Where more do than can be compared with each other (equal logits, or a lane that has many of the
+// greatest), the same is done with those that `found` took, whichever these are, until they are few: the bound rises each time.  (A row of 131072 equal
+// logits, 20 alternatives: 24 us; with a thousand keys compared with each other it took 60.)
 template <int OF, class Scan>
 __device__ int find_top(TopLds<OF>& l, int turn, int top, Scan scan) {
   constexpr int kFull = TopLds<OF>::kCandidates;
@@ -262,20 +280,29 @@ __device__ int find_top(TopLds<OF>& l, int turn, int top, Scan scan) {
   for (;;) {
     scan(bound);
     __syncthreads();
-    const int n = l.count[turn];
-    if (n <= kFull) return n;
-    constexpr int kLanes = kFull / 4 / 64;
-    uint64_t k[kLanes];
+    int n = l.count[turn];
+    if (n <= OF) return n;
+    const bool all = n <= kFull;
+    bound = raised_bound(l, all ? n : kFull, top);
+    uint64_t mine[kFull / OF];
 #pragma unroll
-    for (int w = 0; w < kLanes; ++w) {
-      const uint64_t* const f = l.found + (w * 64 + lane) * 4;
-      const uint64_t a = f[0] > f[1] ? f[0] : f[1], b = f[2] > f[3] ? f[2] : f[3];
-      k[w] = a > b ? a : b;
-    }
-    bound = reached_by<64, 64>(k, top);
+    for (int q = 0; q < kFull / OF; ++q) mine[q] = all && tid + q * OF < n ? l.found[tid + q * OF] : 0;
     __syncthreads();
     if (tid == 0) l.count[turn] = l.stretches[turn] = 0;
     __syncthreads();
+    if (!all) continue;
+    while (true) {       // those that reach the raised bound, until they are few
+#pragma unroll
+      for (int q = 0; q < kFull / OF; ++q)
+        if (mine[q] >= bound) add_found(l, turn, mine[q]);
+      __syncthreads();
+      n = l.count[turn];
+      if (n <= OF) return n;
+      bound = raised_bound(l, n, top);
+      __syncthreads();
+      if (tid == 0) l.count[turn] = 0;
+      __syncthreads();
+    }
   }
 }
 // the logit of a key
