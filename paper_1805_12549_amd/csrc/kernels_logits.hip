@@ -262,12 +262,13 @@ __device__ __forceinline__ uint64_t raised_bound(const TopLds<OF>& l, int n, int
 }
 
 // The `top` < OF greatest keys of a workgroup's lanes, which are all different: found[0, n) holds them, and few others, at most OF in all.  scan(bound) calls
-// add_found for every key from `bound` up, or for more than kCandidates of them.  The top-th of the lanes' greatest keys, cut to 16 bits, is a bound that
+// add_found for every key from `bound` up, or for more than kCandidates of them.  least_key: one that `top` keys reach in any case, for rows in which fewer
+// than `top` lanes have a greater logit than -inf: whatever else there is, classes of -inf among the first 2 * top fill the rest.  The top-th of the lanes' greatest keys, cut to 16 bits, is a bound that
 // at least `top` keys reach; as a rule few more do.  Where more do than can be compared with each other (equal logits, or a lane that has many of the
 // greatest), the same is done with those that `found` took, whichever these are, until they are few: the bound rises each time.  (A row of 131072 equal
 // logits, 20 alternatives: 24 us; with a thousand keys compared with each other it took 60.)
 template <int OF, class Scan>
-__device__ int find_top(TopLds<OF>& l, int turn, int top, Scan scan) {
+__device__ int find_top(TopLds<OF>& l, int turn, int top, uint64_t least_key, Scan scan) {
   constexpr int kFull = TopLds<OF>::kCandidates;
   const int tid = (int)threadIdx.x, lane = tid & 63;
   uint64_t bound;
@@ -277,6 +278,7 @@ __device__ int find_top(TopLds<OF>& l, int turn, int top, Scan scan) {
     for (int w = 0; w < OF / 64; ++w) k[w] = l.lane[turn][w * 64 + lane];
     bound = (uint64_t)reached_by<16, 32>(k, top) << 32;
   }
+  if (bound && (bound >> 32) < 0x00800000u) bound = least_key;
   for (;;) {
     scan(bound);
     __syncthreads();
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(OF) void logprobs_kernel(LogprobArgs a) {
     if (PART) {
       if (tid == 0) a.parts[i] = o;
       if (!a.top) continue;
-      const int n = bad ? 0 : find_top(top, turn, a.top, scan);
+      const int n = bad ? 0 : find_top(top, turn, a.top, rank_key(-INFINITY, (uint32_t)((seg ? z.from : 0) + 2 * a.top - 1)), scan);
       uint64_t* const keys = a.keys + row * segs * a.top + seg;
       for (int k = tid; k < n; k += OF) {
         const int r = rank_among(top.found, n, top.found[k]);
@@ -468,7 +470,7 @@ __global__ __launch_bounds__(OF) void logprobs_kernel(LogprobArgs a) {
       for (int k = n + tid; k < a.top; k += OF) keys[k * segs] = 0;
     } else {
       answer.put(o);
-      if (a.top && !bad) answer.put_top(top.found, find_top(top, turn, a.top, scan));
+      if (a.top && !bad) answer.put_top(top.found, find_top(top, turn, a.top, rank_key(-INFINITY, (uint32_t)(2 * a.top - 1)), scan));
     }
   }
 }
@@ -493,7 +495,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) 
       for (int k = tid; k < n_keys && mine >= bound; k += kThreads)
         if (keys[k] && keys[k] >= bound) add_found(top, turn, keys[k]);
     };
-    answer.put_top(top.found, find_top(top, turn, a.top, scan));
+    answer.put_top(top.found, find_top(top, turn, a.top, 1, scan));
   }
 }
 

@@ -110,6 +110,22 @@ def test_logprobs_of_special_rows(classes, dtype):
     check_logprobs(z, labels, min(128, classes))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes,top", [(50, 20), (300, 128), (1000, 20), (5003, 128), (131072, 20), (140001, 128)])
+def test_logprobs_where_a_mask_leaves_few(classes, top, dtype):
+    """Fewer classes than alternatives, as many and some more, at the row's ends and anywhere: the rest are ruled out ones, by index."""
+    rng = np.random.default_rng(classes)
+    left = [0, 1, 2, top - 1, top, top + 1, 2 * top, classes]
+    z = rows_of(rng, 2 * len(left), classes, dtype)
+    for r, n in enumerate(left * 2):
+        n = min(n, classes)
+        keep = rng.choice(classes, n, replace=False) if r < len(left) else np.r_[:n // 2, classes - (n - n // 2):classes]
+        mask = torch.ones(classes, dtype=torch.bool, device="cuda")
+        mask[torch.from_numpy(keep).cuda()] = False
+        z[r, mask] = -INF
+    check_logprobs(z, rng.integers(0, classes, (2 * len(left),)), top)
+
+
 @pytest.mark.parametrize("classes", [1000, 40000, 131072])
 def test_logprobs_where_one_lane_holds_the_alternatives(classes):
     """The greatest logits at a fixed distance from each other: whichever way a row is shared out, some lane holds many of them."""
