@@ -690,7 +690,7 @@ struct Named {
     if (at < 0) return;
     float minus = 0.0f;
     if (t.taught) {
-#pragma unroll 1
+#pragma unroll 2
       for (int k = 0; k < a.top; k += 4) {       // (entries behind the last one are absent)
         const int4 ids = *(const int4*)(l.id + k);
         const float4 q = *(const float4*)(l.q + k);
