@@ -451,7 +451,8 @@ class GatedConv:
 
 
 # ----------------------------------------------------------------------------
-# The operators behind the classifier, on tensors.  Still marshalling only.
+# The operators behind the classifier, on tensors.  Still marshalling only: torch's autograd does not see these calls (the gradient that
+# distill returns goes into logits.backward(grad)), and they run on the current device's current stream.
 # ----------------------------------------------------------------------------
 
 _LOGITS = {torch.float32: CG_F32, torch.bfloat16: CG_BF16}
