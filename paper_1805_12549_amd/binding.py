@@ -474,6 +474,8 @@ def _logits_of(name, logits):
     (rows, classes), (stride, step) = logits.shape, logits.stride()
     if step != 1 and classes > 1:
         _refuse(name, "the classes of a row must lie side by side")
+    if classes > 0x7fffffff:
+        _refuse(name, "at most 2^31 - 1 classes", CG_EUNSUPPORTED)
     return dtype, rows, classes, stride
 
 
@@ -489,8 +491,8 @@ def _beside(name, what, t, dtype, shape, device):
 def logprobs(logits, labels=None, top: int = 0, temperature: float = 1.0, entropy: bool = True):
     """Log probabilities log softmax(logits / temperature): (logprob, entropy, top_ids, top_logprobs), None for what is not asked for.
 
-    logits: [rows, classes], float32 or bfloat16, any distance between rows.  labels: int64 [rows] or [rows, given], the classes whose log
-    probability is wanted (logprob has their shape; negative: absent, 0).  top: so many alternatives per row in falling order, equal ones by
+    logits: [rows, classes], float32 or bfloat16, any distance between rows; every other tensor contiguous.  labels: int64 [rows] or [rows, given], the
+    classes whose log probability is wanted (logprob has their shape; negative: absent, 0).  top: so many alternatives per row in falling order, equal ones by
     index (int64 and float32 [rows, top]).  entropy: float32 [rows].  See cg_logprobs in cg_conv.h for rows of -inf, NaN and +inf."""
     if _calls is not None:
         out = _calls.logprobs(logits, labels, top, temperature, entropy)
@@ -506,6 +508,8 @@ def logprobs(logits, labels=None, top: int = 0, temperature: float = 1.0, entrop
         if labels.dim() not in (1, 2) or labels.shape[0] != rows:
             _refuse("logprobs", "labels are [rows] or [rows, given]")
         given = 1 if labels.dim() == 1 else labels.shape[1]
+        if given > 0x7fffffff:
+            _refuse("logprobs", "at most 2^31 - 1 labels a row", CG_EUNSUPPORTED)
         logprob = _empty(labels.shape, dtype=torch.float32, device=dev)
     labels_ptr = _beside("logprobs", "labels", labels, torch.int64, None if labels is None else labels.shape, dev)
     if not 0 <= top <= classes:
@@ -556,8 +560,8 @@ def distill(logits, top_ids, top_logits, labels=None, *, teacher_weight: float =
     """Distillation from a teacher's top logits: (loss, stats, grad), one loss per row:
     label_weight * -log softmax(logits)[label] + teacher_weight * KL(softmax(top_logits / temperature) || softmax(logits / temperature)).
 
-    logits: [rows, classes], float32 or bfloat16, any distance between rows.  top_ids, top_logits: int64 and float32 [rows, top], negative ids
-    are absent (both may be None with teacher_weight=0).  labels: int64 [rows], negative: absent.  grad=True: the gradient with respect to the
+    logits (and a given grad): [rows, classes], float32 or bfloat16, any distance between rows; every other tensor contiguous.  top_ids, top_logits: int64
+    and float32 [rows, top], negative ids are absent (both may be None with teacher_weight=0).  labels: int64 [rows], negative: absent.  grad=True: the gradient with respect to the
     logits as well, in the same call (a tensor: into that one, the logits themselves too), times grad_loss (float32 [rows], None: 1).
     stats: what distill_backward takes for the same gradient later on.  The usual factor temperature^2 is the caller's to put into
     teacher_weight.  See cg_distill_forward in cg_conv.h for rows of -inf, NaN and +inf and for labels and ids outside the classes."""

@@ -1004,14 +1004,15 @@ void launch_held(const DistillArgs& a, int64_t chunks, hipStream_t s) {
     hipLaunchKernelGGL((distill_held_kernel<T, TWO, 1024>), grid, dim3(1024), 0, s, a);
 }
 
-// a.segs parts a row by workgroups of 256 threads; whole rows also by wavefronts, and long ones that do not fill the compute units by 512 threads (256 rows of
-// 131072 classes in bf16, the loss alone, 14.4 us and 19.2 on 256; 128 rows of 32768 5.8 and 8.0; 512 rows of 32768 10.6 and 10.6, 768 rows 15.5 and 12.8).
+// a.segs parts a row by workgroups of 256 threads; whole rows also by wavefronts, and long ones that do not fill the compute units by 512 threads (the loss alone, bf16:
+// 256 rows of 131072 classes 14.4 us and 19.2 on 256 threads, 128 rows of 32768 5.8 and 8.0, 512 rows of 32768 10.7 and 10.8, at two temperatures 11.8 and 12.6,
+// 768 rows of 32768 15.5 and 12.8).
 template <class T, bool TWO>
 void launch_rows_of(const DistillArgs& a, int64_t chunks, hipStream_t s) {
   const dim3 grid(row_groups(a.rows * a.segs));
   if (a.segs == 1 && wavefront_each(a.rows, chunks))
     hipLaunchKernelGGL((distill_kernel<T, TWO, 64>), grid, dim3(64), 0, s, a);
-  else if (a.segs == 1 && !a.n_parts && a.rows <= 256 && chunks >= 2 * kPart)
+  else if (a.segs == 1 && !a.n_parts && a.rows <= 512 && chunks >= 2 * kPart)
     hipLaunchKernelGGL((distill_kernel<T, TWO, 512>), grid, dim3(512), 0, s, a);
   else
     hipLaunchKernelGGL((distill_kernel<T, TWO, 256>), grid, dim3(256), 0, s, a);
