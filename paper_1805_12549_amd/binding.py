@@ -562,7 +562,8 @@ def distill(logits, top_ids, top_logits, labels=None, *, teacher_weight: float =
 
     logits (and a given grad): [rows, classes], float32 or bfloat16, any distance between rows; every other tensor contiguous.  top_ids, top_logits: int64
     and float32 [rows, top], negative ids are absent (both may be None with teacher_weight=0).  labels: int64 [rows], negative: absent.  grad=True: the gradient with respect to the
-    logits as well, in the same call (a tensor: into that one, the logits themselves too), times grad_loss (float32 [rows], None: 1).
+    logits as well, in the same call (a tensor: into that one, the logits themselves too), times grad_loss (float32 [rows], None: 1).  Rows of a new
+    gradient are aligned to 16 bytes as the logits' are, with up to 14 bytes between them where the logits' have gaps.
     stats: what distill_backward takes for the same gradient later on.  The usual factor temperature^2 is the caller's to put into
     teacher_weight.  See cg_distill_forward in cg_conv.h for rows of -inf, NaN and +inf and for labels and ids outside the classes."""
     name = "distill"
