@@ -47,7 +47,7 @@ def calls_command(out, lib_dir) -> list:
             "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, '-DCG_TORCH_VERSION="%s"' % torch.__version__, "-isystem", str(home / "include"),
             "-isystem", str(home / "include" / "torch" / "csrc" / "api" / "include"), "-isystem", str(rocm / "include"),
             "-isystem", sysconfig.get_paths()["include"], "-I", str(ROOT / "include"), "-I", str(CSRC), str(CSRC / "py_calls.cpp"), "-o", str(out),
-            "-L", str(home / "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-L", str(lib_dir), "-lcg_conv", "-Wl,-rpath,$ORIGIN"]
+            "-L", str(home / "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-L", str(lib_dir), "-lcg_conv", "-Wl,-rpath,$ORIGIN"]
 
 
 def build(verbose: bool = False, extra=(), jobs: int = 6) -> Path:

@@ -8,7 +8,9 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/hip/HIPContextLight.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -158,7 +160,11 @@ struct Logits {
     rows = t->size(0), classes = t->size(1), stride = t->stride(0);
     return classes > 0 && classes <= INT32_MAX && (classes == 1 || t->stride(1) == 1);
   }
-  at::TensorOptions like(at::ScalarType type) const { return at::TensorOptions().device(t->device()).dtype(type); }
+  // A contiguous tensor on the current device, where the logits are, in memory of its own: it is kept and saved without the call's others.  From torch's
+  // allocator directly: the way through the dispatcher costs each 0.2 us more of host time (one image's answer of four tensors 5.4 us, by at::empty 6.2).
+  at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type) const {
+    return at::detail::empty_generic(sizes, at::cuda::getCUDADeviceAllocator(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
+  }
   // a contiguous tensor of that type beside the logits, or None
   bool beside(PyObject* o, at::ScalarType type, at::IntArrayRef sizes, const void*& ptr) const {
     if (o == Py_None) return true;
@@ -174,31 +180,13 @@ struct Logits {
   bool gradient(PyObject* o, at::Tensor& grad) const {
     if (o == Py_None || o == Py_True) {
       const int64_t step = classes + (((stride - classes) % (dtype == CG_F32 ? 4 : 8)) + 8) % (dtype == CG_F32 ? 4 : 8);
-      grad = at::empty_strided({rows, classes}, {step, 1}, like(t->scalar_type()));
+      grad = at::empty_strided({rows, classes}, {step, 1}, at::TensorOptions().device(t->device()).dtype(t->scalar_type()));
       return true;
     }
     if (!plain_tensor(o)) return false;
     grad = THPVariable_Unpack(o);
     return !grad.unsafeGetTensorImpl()->has_symbolic_sizes_strides() && grad.scalar_type() == t->scalar_type() && grad.sizes() == t->sizes() &&
            grad.device() == t->device() && (classes == 1 || grad.stride(1) == 1);
-  }
-};
-
-// The small outputs of a call in one block, which lives as long as one of them does: an allocation of its own costs each 0.8 us of host time, of some six
-// that a call takes.
-struct Block {
-  at::Tensor all;
-  int64_t used = 0;
-  static int64_t room(int64_t count, int64_t size) { return (count * size + 63) & ~(int64_t)63; }
-  Block(const Logits& z, int64_t bytes) : all(at::empty({bytes}, z.like(at::kByte))) {}
-  // a contiguous tensor of the next room(...) bytes
-  at::Tensor take(at::IntArrayRef sizes, at::ScalarType type) {
-    const caffe2::TypeMeta meta = at::scalarTypeToTypeMeta(type);
-    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.unsafeGetTensorImpl()->key_set(), meta);
-    t.unsafeGetTensorImpl()->set_storage_offset(used / (int64_t)meta.itemsize());
-    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
-    used += room(t.numel(), (int64_t)meta.itemsize());
-    return t;
   }
 };
 
@@ -246,13 +234,11 @@ PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   {
     const WithoutGil released;
     const hipStream_t stream = c10::hip::getCurrentHIPStream().stream();
-    Block block(z, (labels ? Block::room(z.rows * given, 4) : 0) + (entropy_wanted ? Block::room(z.rows, 4) : 0) + Block::room(z.rows * top, 8) +
-                       Block::room(z.rows * top, 4));
-    if (labels) logprob = block.take(labels->sizes(), at::kFloat);
-    if (entropy_wanted) entropy = block.take({z.rows}, at::kFloat);
+    if (labels) logprob = z.fresh(labels->sizes(), at::kFloat);
+    if (entropy_wanted) entropy = z.fresh({z.rows}, at::kFloat);
     if (top) {
-      top_ids = block.take({z.rows, top}, at::kLong);
-      top_logprobs = block.take({z.rows, top}, at::kFloat);
+      top_ids = z.fresh({z.rows, top}, at::kLong);
+      top_logprobs = z.fresh({z.rows, top}, at::kFloat);
     }
     const size_t need = cg_logprobs_workspace_bytes(z.rows, (int32_t)z.classes, (int32_t)top);
     const Scratch scratch(need, stream);
@@ -312,9 +298,8 @@ PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
                                (int32_t)top, (const int64_t*)labels, w_teacher, w_label, (const float*)given_stats, (const float*)up, grad.data_ptr(),
                                grad.stride(0), stream);
     } else {
-      Block block(z, Block::room(z.rows, 4) + Block::room(z.rows * 3, 4));
-      loss = block.take({z.rows}, at::kFloat);
-      stats = block.take({z.rows, 3}, at::kFloat);
+      loss = z.fresh({z.rows}, at::kFloat);
+      stats = z.fresh({z.rows, 3}, at::kFloat);
       const size_t need = cg_distill_workspace_bytes(z.rows, (int32_t)z.classes);
       const Scratch scratch(need, stream);
       rc = cg_distill_forward(z.t->data_ptr(), z.dtype, z.rows, (int32_t)z.classes, z.stride, temperature, (const int64_t*)ids, (const float*)top_logits,
