@@ -176,11 +176,13 @@ struct Logits {
     ptr = b.data_ptr();
     return true;
   }
-  // where the gradient goes: None or True (a new tensor whose rows are aligned to 16 bytes as the logits' are) or a tensor
+  // where the gradient goes: None or True (a new tensor, each of whose rows is aligned to 16 bytes as the logits' row is) or a tensor
   bool gradient(PyObject* o, at::Tensor& grad) const {
     if (o == Py_None || o == Py_True) {
-      const int64_t step = classes + (((stride - classes) % (dtype == CG_F32 ? 4 : 8)) + 8) % (dtype == CG_F32 ? 4 : 8);
-      grad = at::empty_strided({rows, classes}, {step, 1}, at::TensorOptions().device(t->device()).dtype(t->scalar_type()));
+      const int64_t size = dtype == CG_F32 ? 4 : 2, per = 16 / size, step = classes + ((stride - classes) % per + per) % per;
+      const int64_t phase = rows ? (int64_t)((uintptr_t)t->data_ptr() % 16) / size : 0;
+      grad = fresh({rows ? phase + (rows - 1) * step + classes : 0}, t->scalar_type());
+      grad.unsafeGetTensorImpl()->set_sizes_and_strides(t->sizes(), at::IntArrayRef{step, 1}, phase);
       return true;
     }
     if (!plain_tensor(o)) return false;
