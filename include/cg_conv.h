@@ -259,7 +259,7 @@ enum { CG_TOP_MAX = 128 }; /* the most alternatives, and the most classes of a t
  *   entropy       nullable, [rows]: -sum p log p
  *   top_ids, top_logprobs  [rows][top]: the `top` classes of the greatest logits in falling order, equal ones (0 and -0 too) by
  *                 rising index; 0 <= top <= min(classes, CG_TOP_MAX); nullable if top == 0
- * A class of -inf has probability 0 (log -inf).  A row of -inf throughout has log probabilities -inf, entropy 0 and its first
+ * A class of -inf has probability 0 (log -inf), and a log probability below float32's range is -inf.  A row of -inf throughout has log probabilities -inf, entropy 0 and its first
  * classes as alternatives.  A row with a NaN or +inf has no distribution: NaN in the place of log probabilities (other than those of
  * absent labels) and entropy, -1 in the place of top_ids. */
 size_t cg_logprobs_workspace_bytes(int64_t rows, int32_t classes, int32_t top);

@@ -1,8 +1,8 @@
 // What is done with the logits behind the classifier: log probabilities of given classes with the entropy and the top alternatives
 // (cg_logprobs), and the distillation loss from a teacher's top logits with its gradient (cg_distill_forward, cg_distill_backward).
 //
-// With m = max z and c = 1 / temperature every quantity is formed from the differences (z - m) * c: neither a large offset of a row nor logits at the
-// type's lowest value cost precision or overflow.  Probabilities are e / sum, not exponentials of a difference from a rounded logarithm.  All sums are held in 32
+// With m = max z and c = 1 / temperature every quantity is formed from the differences, as (z - m) / 2 * 2 c: neither a large offset of a row nor logits at
+// the type's ends cost precision or overflow.  Probabilities are e / sum, not exponentials of a difference from a rounded logarithm.  All sums are held in 32
 // bits; only a gradient is rounded to the logits' type, once.  An element costs an exponential and some ten other instructions, so that from a few hundred
 // rows on memory bounds every call but those of two temperatures at once.
 #include <hip/hip_runtime.h>
@@ -40,6 +40,10 @@ __device__ __forceinline__ uint64_t rank_key(float z, uint32_t index) {
 
 // exp2 by the hardware (one ulp; results below 2^-126 are 0)
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// (x - from) / 2, of which the factors below take twice the reciprocal temperature: the difference of two logits may pass the range of 32 bits where that over
+// the temperature does not.  One fma, rounded as the difference is.
+__device__ __forceinline__ float half_apart(float x, float from) { return fmaf(x, 0.5f, -0.5f * from); }
 
 // A row as the lanes of a workgroup walk it: elements in front of the first 16-byte boundary, whole 16-byte chunks, elements behind the last one; or
 // part `seg` of `segs` of its chunks, the elements beside them with the first part.
@@ -125,13 +129,13 @@ __device__ __forceinline__ void load_chunks(const RowSpan<T>& z, int first, uint
   }
 }
 
-// A softmax in one pass: with m the greatest logit so far, the sum of e = 2^((z - m) c) and the sum of e (z - m) c, c = log2(e) / temperature.
+// A softmax in one pass: with m the greatest logit so far, the sum of e = 2^y and the sum of e y, y = (z - m) / 2 * c, c = 2 log2(e) / temperature.
 // A new maximum scales both.  NaN and +inf make the sum NaN; without any class m is -inf and the sum 0.
 struct Online {
   float m, sum, moment;
   // to the maximum `to` >= m
   __device__ void raise(float to, float c) {
-    const float d = fmaxf((m - to) * c, kLeast), f = pow2(d);
+    const float d = fmaxf(half_apart(m, to) * c, kLeast), f = pow2(d);
     moment = f * (moment + d * sum);
     sum *= f;
     m = to;
@@ -142,7 +146,7 @@ struct Online {
     const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float y = (x[i] - from) * c, e = pow2(y);
+      const float y = half_apart(x[i], from) * c, e = pow2(y);
       sum += e;
       moment = fmaf(e, fmaxf(y, kLeast), moment);
     }
@@ -364,7 +368,7 @@ struct RowAnswer {
     if (a.entropy && tid == 0) a.entropy[row] = none ? 0.0f : log_sum - o.moment / (o.sum * kLog2E);
     for (int k = tid; bad && k < a.top; k += OF) put_top(k, -1, NAN);
   }
-  __device__ float of(float x) const { return none ? -INFINITY : bad ? NAN : (x - m) * a.scale - log_sum; }
+  __device__ float of(float x) const { return none ? -INFINITY : bad ? NAN : half_apart(x, m) * (2.0f * a.scale) - log_sum; }
   __device__ void put_top(int at, int64_t id, float logprob) const {
     a.top_ids[row * a.top + at] = id;
     a.top_logprobs[row * a.top + at] = logprob;
@@ -388,7 +392,7 @@ __global__ __launch_bounds__(OF) void logprobs_kernel(LogprobArgs a) {
   __shared__ TopLds<OF> top;
   constexpr int N = RowSpan<T>::kPer, kMarks = TopLds<OF>::kMarks;
   const int tid = (int)threadIdx.x, segs = PART ? a.segs : 1;
-  const float c = a.scale * kLog2E;
+  const float c = 2.0f * a.scale * kLog2E;
   int turn = 0;
   for (long long i = blockIdx.x; i < a.rows * segs; i += gridDim.x, turn ^= 1) {
     const long long row = PART ? i / segs : i;
@@ -489,7 +493,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) 
     uint64_t mine = 0;
     for (int k = tid; k < n_keys; k += kThreads) mine = keys[k] > mine ? keys[k] : mine;
     if (a.top) offer_lane(top, turn, (uint32_t)(mine >> 32));
-    answer.put(join_parts(a.parts + row * a.segs, a.segs, Online{-INFINITY, 0.0f, 0.0f}, a.scale * kLog2E));
+    answer.put(join_parts(a.parts + row * a.segs, a.segs, Online{-INFINITY, 0.0f, 0.0f}, 2.0f * a.scale * kLog2E));
     if (!a.top) continue;
     __syncthreads();
     if (answer.bad) continue;
@@ -548,7 +552,7 @@ __device__ __forceinline__ void take_teacher(TeacherLds& l, const DistillArgs& a
   float e[kEach];
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    t[k] = (t[k] - most) * a.scale;
+    t[k] = half_apart(t[k], most) * (2.0f * a.scale);
     e[k] = pow2(t[k] * kLog2E);
     mass += e[k];
   }
@@ -568,13 +572,14 @@ __device__ __forceinline__ void take_teacher(TeacherLds& l, const DistillArgs& a
   if (lane == 0) l.beyond = beyond;
 }
 
-// A row's sums for the one or two temperatures of a call: m the greatest logit, `sum` of 2^((z - m) c), `sum1` (TWO) of 2^((z - m) log2 e).
+// A row's sums for the one or two temperatures of a call: m the greatest logit, `sum` of 2^((z - m) / 2 * c), `sum1` (TWO) of 2^((z - m) log2 e).
 template <bool TWO>
 struct Sums {
   float m, sum, sum1;
   __device__ void raise(float to, float c) {
-    sum *= pow2(fmaxf((m - to) * c, kLeast));
-    if (TWO) sum1 *= pow2(fmaxf((m - to) * kLog2E, kLeast));
+    const float d = half_apart(m, to);
+    sum *= pow2(fmaxf(d * c, kLeast));
+    if (TWO) sum1 *= pow2(fmaxf(d * (2.0f * kLog2E), kLeast));
     m = to;
   }
   template <int N>
@@ -583,8 +588,9 @@ struct Sums {
     const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      sum += pow2((x[i] - from) * c);
-      if (TWO) sum1 += pow2((x[i] - from) * kLog2E);
+      const float d = half_apart(x[i], from);
+      sum += pow2(d * c);
+      if (TWO) sum1 += pow2(d * (2.0f * kLog2E));
     }
   }
   __device__ void add(const Sums& b) {
@@ -608,7 +614,7 @@ __device__ __forceinline__ uint4 pack(const float* g, const uint16_t*) {
 }
 
 // The exponentials' factor of the first sum (the only one, or the teacher's).
-__device__ __forceinline__ float first_factor(const DistillArgs& a) { return a.w_teacher != 0.0f ? a.scale * kLog2E : kLog2E; }
+__device__ __forceinline__ float first_factor(const DistillArgs& a) { return 2.0f * kLog2E * (a.w_teacher != 0.0f ? a.scale : 1.0f); }
 
 template <class T, int kOf, bool TWO>
 __device__ __forceinline__ void take_chunks(Sums<TWO>& o, const uint4* raw, float c) {
@@ -662,8 +668,8 @@ struct Terms {
   }
   // the probabilities' part of a class's gradient
   __device__ float slope(float x) const {
-    const float y = x - m, p = kt * pow2(y * c);
-    return none ? 0.0f : TWO ? fmaf(k1, pow2(y * kLog2E), p) : p;
+    const float y = half_apart(x, m), p = kt * pow2(y * c);
+    return none ? 0.0f : TWO ? fmaf(k1, pow2(y * (2.0f * kLog2E)), p) : p;
   }
 };
 
@@ -673,7 +679,7 @@ __device__ __forceinline__ void put_loss(const DistillArgs& a, long long row, co
   const float log_sum = logf(o.sum);
   float loss = 0.0f;
   for (int k = (int)threadIdx.x; k < a.top && t.taught; k += 64)
-    if (l.q[k] != 0.0f) loss += l.q[k] * (l.log_q[k] - ((l.z[k] - o.m) * a.scale - log_sum));
+    if (l.q[k] != 0.0f) loss += l.q[k] * (l.log_q[k] - (half_apart(l.z[k], o.m) * (2.0f * a.scale) - log_sum));
   loss = sum_over_lanes(loss);
   loss = t.taught ? loss * t.wt : 0.0f;
   if (t.labelled) loss += t.wl * ((TWO ? logf(o.sum1) : log_sum) - (l.z_label - o.m));
@@ -910,7 +916,7 @@ int check_logits(const char* who, const void* logits, int32_t dtype, int64_t row
   if (rows < 0 || classes <= 0) return cg::set_error(CG_EINVAL, "%s: bad size", who);
   if (dtype != CG_F32 && dtype != CG_BF16) return cg::set_error(CG_EUNSUPPORTED, "%s: logits are CG_F32 or CG_BF16", who);
   if (row_stride < 0) return cg::set_error(CG_EINVAL, "%s: row_stride must not be negative", who);
-  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isnormal(1.0f / temperature) || !std::isfinite(1.0f / temperature * kLog2E))
+  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isnormal(1.0f / temperature) || !std::isfinite(2.0f / temperature * kLog2E))
     return cg::set_error(CG_EINVAL, "%s: temperature must be positive and lie between 2^-126 and 2^126", who);
   if (rows > 0 && row_stride > (int64_t)((1ull << 62) / (uint64_t)rows)) return cg::set_error(CG_EINVAL, "%s: bad size", who);
   if (rows > 0 && !logits) return cg::set_error(CG_EINVAL, "%s: logits must not be NULL", who);
