@@ -272,7 +272,8 @@ int cg_logprobs(const void* logits, int32_t dtype, int64_t rows, int32_t classes
  * with p1 = softmax(logits), pT = softmax(logits / temperature) over all classes and q = softmax(top_logits / temperature)
  * over the row's `top` teacher classes (any constant may be added to a row of top_logits: log probabilities will do).
  *   top_ids, top_logits  [rows][top], top <= CG_TOP_MAX.  A negative id is absent; so lists may be ragged.  A class named twice counts
- *                 with both entries.  top_logits of -inf hold no mass.  Nullable if top == 0 (teacher_weight must then be 0).
+ *                 with both entries.  top_logits of -inf hold no mass, nor do those whose exp((top_logit - the greatest) / temperature) is below
+ *                 2^-126 (87.3 temperatures down), whatever their class's logit.  Nullable if top == 0 (teacher_weight must then be 0).
  *   labels        [rows], negative: absent.  Nullable if label_weight is 0.
  * A term whose weight is 0, whose label is absent or whose teacher has no mass is left out of its row.  A row without terms, and a row of
  * -inf throughout, has loss 0 and gradient 0, whatever else it holds.  A label or id of `classes` or more makes the loss and the

@@ -77,3 +77,16 @@ def test_far_logits_and_a_far_teacher(classes, dtype, temperature):
             O.check(got[r].item(), lv, lb, "row %d loss" % r)
         for got in (grad, later):
             O.check(got[r].double().cpu().numpy(), gv, gb, "row %d gradient" % r)
+
+
+def test_a_teachers_entry_below_the_normal_range_holds_no_mass():
+    """87.3 temperatures below the greatest one: such an entry asks for nothing, of a class that is ruled out neither; above that the loss is infinite."""
+    z = torch.zeros((4, 1000), device="cuda")
+    z[:, 7] = -float("inf")
+    ids = torch.tensor([[3, 7]] * 4, device="cuda")
+    t = torch.tensor([[0.0, -87.0], [0.0, -88.0], [5.0, -3.0e38], [0.0, -float("inf")]], device="cuda")
+    for temperature in (1.0, 4.0):
+        loss, _, grad = B.distill(z, ids, t * temperature if temperature == 1.0 else torch.where(t > -1e38, t * temperature, t), temperature=temperature, grad=True)
+        assert loss[0].item() == float("inf")
+        assert np.abs(loss[1:].cpu().numpy() - np.log(999.0)).max() <= (O.chain(1000) + 64) * O.U * np.log(999.0)
+        assert torch.isfinite(grad).all() and (grad[1:, 7] == 0).all()
