@@ -3,8 +3,9 @@
 //
 // With m = max z and c = 1 / temperature every quantity is formed from the differences, as (z - m) / 2 * 2 c: neither a large offset of a row nor logits at
 // the type's ends cost precision or overflow.  Probabilities are e / sum, not exponentials of a difference from a rounded logarithm.  All sums are held in 32
-// bits; only a gradient is rounded to the logits' type, once.  An element costs an exponential and some ten other instructions, so that from a few hundred
-// rows on memory bounds every call but those of two temperatures at once.
+// bits; only a gradient is rounded to the logits' type, once.  An element costs an exponential and some ten other instructions, so that memory bounds
+// calls of a few hundred long rows (2048 of 50003 classes in bf16: 4.8 TB/s read), but for the loss alone at two temperatures (2048 of 32000 in fp32: 3.5 TB/s).  Rows
+// of a few KB are bound by their latencies (the loss of 4096 rows of 1000 in fp32: 2.1 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -268,10 +269,13 @@ __device__ __forceinline__ uint64_t raised_bound(const TopLds<OF>& l, int n, int
 
 // The `top` < OF greatest keys of a workgroup's lanes, which are all different: found[0, n) holds them, and few others, at most OF in all.  scan(bound) calls
 // add_found for every key from `bound` up, or for more than kCandidates of them.  least_key: one that `top` keys reach in any case, for rows in which fewer
-// than `top` lanes have a greater logit than -inf: whatever else there is, classes of -inf among the first 2 * top fill the rest.  The top-th of the lanes' greatest keys, cut to 16 bits, is a bound that
-// at least `top` keys reach; as a rule few more do.  Where more do than can be compared with each other (equal logits, or a lane that has many of the
-// greatest), the same is done with those that `found` took, whichever these are, until they are few: the bound rises each time.  (256 rows of 1000 equal
-// logits, 20 alternatives: 14 us; with a thousand keys compared with each other 64.)
+// than `top` lanes have a greater logit than -inf: whatever else there is, classes of -inf among the first 2 * top fill the rest.  The top-th of the lanes'
+// greatest keys, cut to 16 bits, is a bound that at least `top` keys reach; as a rule few more do.  Where more do than can be compared with each other (equal
+// logits, or a lane that has many of the greatest), the same is done with those that `found` took, whichever these are, until they are few: the bound rises
+// each time.  (256 rows of 1000 equal logits, 20 alternatives: 13 us; with a thousand keys compared with each other 64.)  Dear are rows with fewer chunks than
+// alternatives, which have no bound at first (256 rows of 300 in fp32, 128 alternatives, 13.6 us, of 1000 in bf16 16.0; with 64 alternatives 7.5 and 7.7), and
+// rising rows whose logits share their upper 16 bits, whose bound rises by some thousand keys a scan (129 rows of 65536 in fp32, 20 alternatives, 241 us, equal
+// ones 36, others 16; of 2^20 1356, 211 and 116).
 template <int OF, class Scan>
 __device__ int find_top(TopLds<OF>& l, int turn, int top, uint64_t least_key, Scan scan) {
   constexpr int kFull = TopLds<OF>::kCandidates;
@@ -381,11 +385,12 @@ struct RowAnswer {
   }
 };
 
-// One pass over the row (V elements are read once): every lane keeps its own running maximum and sums.  The alternatives come from what the pass
-// leaves behind: the lanes' maxima give a bound that is reached by little more than `top` classes, the maxima of each lane's stretches say where those
-// lie, and only such stretches are read again, all at once.  PART: a workgroup takes one of `segs` parts of a row, and leaves its sums and keys to
-// logprobs_join_kernel.  4096 rows of 131072 classes in bf16 with 64 alternatives 201 us (5.3 TB/s; without alternatives 192, 5.6), 2048 rows of 50003 43 us: bound
-// by memory.  One row of 1000 classes 4.5 us (3.0 without alternatives): bound by its latencies, launch, loads, two barriers and the comparisons.
+// One pass over the row (V elements are read once): every lane keeps its own running maximum and sums.  The alternatives come from what the pass leaves behind:
+// the lanes' maxima give a bound that is reached by little more than `top` classes, the maxima of each lane's stretches say where those lie, and only such
+// stretches are read again, all at once.  PART: a workgroup takes one of `segs` parts of a row, and leaves its sums and keys to logprobs_join_kernel.  4096
+// rows of 131072 classes in bf16 with 64 alternatives 201 us (5.3 TB/s; without alternatives 192, 5.6), in fp32 401 us (without 364, 5.9 TB/s), 2048 rows of
+// 50003 in bf16 43 us: bound by memory.  One row of 1000 classes 4.5 us (3.0 without alternatives): bound by its latencies, launch, loads, two barriers and the
+// comparisons.
 template <class T, bool PART, int OF>
 __global__ __launch_bounds__(OF) void logprobs_kernel(LogprobArgs a) {
   __shared__ Online part[2][OF / 64];
@@ -808,11 +813,13 @@ __global__ __launch_bounds__(OF) void distill_kernel(DistillArgs a) {
   }
 }
 
-// Loss and gradient in one pass: kHeld chunks a lane stay in the registers of the row's workgroup between the sums and the gradient (256 KB by 1024 threads, half of
-// a compute unit's registers), and as the gradient leaves, the next row's chunks take their place, so that loads and stores are on their way together.  A
-// workgroup walks rows.  What a longer row has beside (1024 threads only) is read twice.  Rows of logits and gradient have the same alignment to 16 bytes.
-// Bound by memory: 4096 rows of 131072 classes in bf16 461 us, 4.66 TB/s of one read and one write an element, where a plain copy reaches 4.83; read
-// twice by distill_kernel they took 647 us.  2048 rows of 131072 in fp32 (twice what is held) 494 and 648 us, of 200003 839 and 1103 us.
+// Loss and gradient in one pass: kHeld chunks a lane stay in the registers of the row's workgroup between the sums and the gradient (256 KB by 1024 threads,
+// half of a compute unit's registers), and as the gradient leaves, the next row's chunks take their place, so that loads and stores are on their way together.
+// A workgroup walks rows.  What a longer row has beside (1024 threads only) is read twice.  Rows of logits and gradient have the same alignment to 16 bytes.
+// Bound by memory: 4096 rows of 131072 classes in bf16 461 us, 4.66 TB/s of one read and one write an element, where a plain copy reaches 4.83 and the gradient
+// from given sums, which moves as much, 5.4; read twice by distill_kernel they took 647 us.  Rows of 50003 in bf16 192 us, by distill_kernel 243 (where a
+// gradient given by the caller has another alignment than the logits).  2048 rows of 131072 in fp32 (twice what is held) 494 and 648 us, of 200003 839 and 1103
+// us.
 constexpr int kHeld = 16, kMore = 2;       // kMore: chunks a lane takes at once of what is beside
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -982,9 +989,9 @@ void launch_logprobs(const LogprobArgs& a, hipStream_t s) {
   }
 }
 
-// Threads of distill_held_kernel for a row: as few as hold it, and more as long as all of them find room at once (1024 threads on each of 256 compute
-// units) and each has four chunks.  32768 classes in bf16: 64 rows 9.6 us on 256 threads, 8.1 on 512, 8.0 on 1024, 512 rows 18.9, 18.0 and 19.3,
-// 1024 rows 32.8, 33.5 and 38.5; 4096 rows of 1000 in fp32 12.1 us on 64 threads and 21.8 on 256.
+// Threads of distill_held_kernel for a row: as few as hold it, and more as long as all of them find room at once (1024 threads on each of 256 compute units)
+// and each has four chunks.  32768 classes in bf16: 64 rows 9.6 us on 256 threads, 8.1 on 512, 8.0 on 1024, 512 rows 18.9, 18.0 and 19.3, 1024 rows 32.8, 33.5
+// and 38.5; rows of 1000 in fp32 on 64 and on 256 threads: 4096 rows 12.4 and 22.5 us, 1024 6.3 and 7.1, 512 5.8 and 5.8, 128 5.4 and 5.2, one 5.0 and 4.8.
 constexpr int64_t kRoom = 256 * 1024;
 int held_threads(int64_t rows, int64_t chunks) {
   int of = 64;
@@ -1010,9 +1017,11 @@ void launch_held(const DistillArgs& a, int64_t chunks, hipStream_t s) {
     hipLaunchKernelGGL((distill_held_kernel<T, TWO, 1024>), grid, dim3(1024), 0, s, a);
 }
 
-// a.segs parts a row by workgroups of 256 threads; whole rows also by wavefronts, and long ones that do not fill the compute units by 512 threads (the loss alone, bf16:
-// 256 rows of 131072 classes 14.4 us and 19.2 on 256 threads, 128 rows of 32768 5.8 and 8.0, 512 rows of 32768 10.7 and 10.8, at two temperatures 11.8 and 12.6,
-// 768 rows of 32768 15.5 and 12.8).
+// a.segs parts a row by workgroups of 256 threads; whole rows also by wavefronts, and long ones by 512 threads up to two rows a compute unit.  On 512 and on
+// 256 threads, bf16: the loss alone, 256 rows of 131072 classes 14.4 and 19.2 us; of 32768 128 rows 5.8 and 8.0, 256 7.3 and 8.5, 384 9.4 and 10.0, 512 10.7
+// and 10.8, 640 14.2 and 12.1; of 16384 128 rows 4.9 and 5.4, 512 7.8 and 8.0; at two temperatures 384 rows of 32768 10.9 and 11.7, 640 15.9 and 14.6.  Loss
+// and gradient at another alignment: 256 rows of 16384 8.5 and 10.2, 384 of 50003 23.4 and 25.9, 512 28.6 and 29.6, 640 43.2 and 40.7.  The gradient alone
+// comes here whole with 512 rows of 16384 to 32767 only: 16384 11.2 and 10.8, 24000 12.7 and 12.9.
 template <class T, bool TWO>
 void launch_rows_of(const DistillArgs& a, int64_t chunks, hipStream_t s) {
   const dim3 grid(row_groups(a.rows * a.segs));
